@@ -325,6 +325,142 @@ rv_status rv_admit_staged_layers(int n_layers, const void *const *Q, const float
                                  int frame_id, float *const *saliency_out, int32_t *const *idx_out,
                                  void *stream);
 
+/* ---- a layer's projections to frame tensors -------------------------------------------
+ *
+ * The step before attention: per token and head, the norm of queries and keys over the head's
+ * 64 elements, then the rotation by the token's position, in one pass over the projections'
+ * outputs, rounded to bf16 once:
+ *   g = x - mean(x) (RV_NORM_LAYER) or x,  r = 1 / sqrt(mean(g^2) + eps),
+ *   y = g r weight + bias   (RV_NORM_NONE: y = x),
+ * and with n_axes > 0 the 64 elements are n_axes blocks of D = 64 / n_axes; in block a the pair
+ * (i, i + D/2), i < D/2, turns by the angle t = pos[a] base^(-2i/D):
+ *   (y_i, y_{i+D/2}) -> (y_i cos t - y_{i+D/2} sin t, y_{i+D/2} cos t + y_i sin t).
+ * Two axes are a patch's row and column in its grid (0, 0 for tokens that have none).  Angles
+ * of any 32-bit position are exact to 2^-32 turns; all arithmetic is fp32. */
+typedef enum rv_norm { RV_NORM_NONE = 0, RV_NORM_RMS = 1, RV_NORM_LAYER = 2 } rv_norm;
+typedef enum rv_dtype { RV_BF16 = 0, RV_F32 = 1 } rv_dtype;
+
+typedef struct rv_qkv_prep {
+    int32_t n_q_heads, n_kv_heads; /* >= 1 */
+    int32_t norm;                  /* rv_norm */
+    int32_t n_axes;                /* 0 (no rotation), 1 or 2 */
+    float eps;                     /* >= 0 */
+    double base;                   /* >= 1, finite (n_axes > 0) */
+    /* device, [64] fp32, each may be NULL (ones, zeros); must be NULL for RV_NORM_NONE */
+    const float *q_weight, *q_bias, *k_weight, *k_bias;
+} rv_qkv_prep;
+
+/* q, k, v: n_tokens rows of q_stride, k_stride, v_stride elements (of `dtype`), head h of a
+ * row at element 64 h, e.g. column ranges of one fused projection.  v and V may both be NULL.
+ * pos: [n_tokens][n_axes] int32 (NULL for n_axes 0).  Q: [n_tokens][n_q_heads][64] bf16; K, V:
+ * [n_tokens][n_kv_heads][64] bf16.  Rows and addresses must be 16-byte aligned
+ * (RV_ERR_INVALID).  The outputs must not overlap the inputs.  n_tokens 0 is a no-op. */
+rv_status rv_prepare_qkv(const rv_qkv_prep *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                         const void *v, int64_t v_stride, rv_dtype dtype, int n_tokens, const int32_t *pos,
+                         void *Q, void *K, void *V, void *stream);
+
+/* rv_prepare_qkv whose K and V are written to the staged rows of m (rv_mem_stage for n_tokens
+ * rows, then the rows): a frame goes from the projections to the arena in one launch.
+ * p->n_kv_heads must be m's head count; v is required.  Errors as rv_mem_stage. */
+rv_status rv_mem_stage_qkv(rv_mem m, const rv_qkv_prep *p, const void *q, int64_t q_stride, const void *k,
+                           int64_t k_stride, const void *v, int64_t v_stride, rv_dtype dtype, int n_tokens,
+                           const int32_t *pos, void *Q, void *stream);
+
+/* The gradients of rv_prepare_qkv.  q, k, pos as given to it; dQ, dK, dV: the gradients of Q, K, V,
+ * laid out as they are (bf16); dq, dk, dv: of `dtype`, rows of dq_stride, ... elements, rounded once.
+ * dV and dv may both be NULL.  dq_weight, dq_bias, dk_weight, dk_bias: [64] fp32, overwritten with
+ * the sums over tokens and heads, in a fixed order (the same inputs give the same bits); each may be
+ * NULL, and must be for RV_NORM_NONE.  n_tokens 0 sets them to zero.  rv_init must have run on the
+ * device: the sums' partial results lie in its workspace. */
+rv_status rv_prepare_qkv_bwd(const rv_qkv_prep *p, const void *q, int64_t q_stride, const void *k,
+                             int64_t k_stride, rv_dtype dtype, int n_tokens, const int32_t *pos, const void *dQ,
+                             const void *dK, const void *dV, void *dq, int64_t dq_stride, void *dk,
+                             int64_t dk_stride, void *dv, int64_t dv_stride, float *dq_weight, float *dq_bias,
+                             float *dk_weight, float *dk_bias, void *stream);
+
+/* ---- sequences in pages ---------------------------------------------------------------
+ *
+ * A pool holds the rows of many sequences of one layer (streams, or continuations of one) in pages
+ * of RV_PAGE_ROWS rows of every head, K and V [n_pages][n_heads][64][64] bf16.  A sequence is a
+ * list of pages; forked sequences share pages, and a page returns to the pool when its last
+ * user drops it.  Rows never move except in rv_pool_compact.  Lengths and lists are kept on the host
+ * as enqueued (no device sync); the device's copy of the lists is written by kernels, in
+ * stream order, so the calls can be captured: a captured call keeps the rows and pages it was
+ * enqueued with.  Calls on one pool must be ordered on one stream.  On failure nothing changes. */
+#define RV_PAGE_ROWS 64
+typedef struct rv_pool_s *rv_pool;
+
+/* A pool of n_pages pages for up to max_seqs open sequences of up to max_rows rows, on the current
+ * device.  head_dim must be 64.  Runs rv_init and allocates everything later calls use, the
+ * partial results of rv_attend_seqs among it (71 MB once per device).  Synchronous. */
+rv_status rv_pool_create(int n_heads, int head_dim, int n_pages, int max_seqs, int64_t max_rows, rv_pool *out);
+
+/* Frees the pool (synchronises its device first).  NULL is accepted. */
+rv_status rv_pool_destroy(rv_pool p);
+
+/* Pages that no sequence uses; -1 for NULL. */
+int rv_pool_free_pages(rv_pool p);
+
+/* A new, empty sequence (RV_ERR_CAPACITY if max_seqs are open). */
+rv_status rv_pool_open(rv_pool p, int *seq);
+
+/* Rows of a sequence as enqueued; -1 if it is not open. */
+int64_t rv_pool_len(rv_pool p, int seq);
+
+/* n new sequences that begin with the first n_rows rows of seq (0 <= n_rows <= its length) and share
+ * their pages with it: no row is copied.  children: host array of n that receives them. */
+rv_status rv_pool_fork(rv_pool p, int seq, int64_t n_rows, int n, int *children, void *stream);
+
+/* Closes n sequences (each named once); pages without another user are free for the next call. */
+rv_status rv_pool_close(rv_pool p, int n, const int *seqs);
+
+/* Drops the newest rows of a sequence: 0 <= n_rows <= its length.  Host-side only. */
+rv_status rv_pool_truncate(rv_pool p, int seq, int64_t n_rows);
+
+/* Appends n_rows[i] rows (0 allowed) to seqs[i], for i < n.  K, V: the rows of all of them one
+ * after another, [sum of n_rows][n_heads][64] bf16 device memory.  A last page that is partly
+ * full and shared is copied first; the other users' rows stay as they are.  A sequence may be
+ * named once.  RV_ERR_CAPACITY if pages or max_rows do not suffice. */
+rv_status rv_pool_append(rv_pool p, int n, const int *seqs, const void *K, const void *V, const int *n_rows,
+                         void *stream);
+
+/* Copies rows first[i] .. first[i] + n_rows[i] - 1 of seqs[i] to the next n_heads n_rows[i] rows of K and
+ * V ([n_heads][n_rows[i]][64] bf16, the layout of a memory, for each i in turn; either may be NULL).
+ * first NULL: from row 0. */
+rv_status rv_pool_gather(rv_pool p, int n, const int *seqs, const int64_t *first, const int64_t *n_rows, void *K,
+                         void *V, void *stream);
+
+/* Keeps rows 0 .. first[i] - 1 of seqs[i] and, after them, per head the n_keep[i] rows that keep names:
+ * keep holds for each i in turn [n_heads][n_keep[i]] int32 row numbers (device memory, any order,
+ * repeats allowed, each in [first[i], length); a number outside gives a row of zeros).  The new
+ * length is first[i] + n_keep[i] <= max_rows.  Full pages before first[i] stay (and stay shared); the
+ * others' kept rows are written to new pages, which must be free while the old ones are still
+ * held (RV_ERR_CAPACITY).  first NULL: 0.  A sequence may be named once. */
+rv_status rv_pool_compact(rv_pool p, int n, const int *seqs, const int64_t *first, const int64_t *n_keep,
+                          const int32_t *keep, void *stream);
+
+/* Attention (Sec. 3.1 Eq. 3) of n_tokens[i] queries over the rows of seqs[i] and, unless K and V
+ * are NULL, over the n_tokens[i] keys that belong to the queries, for i < n; no mask among them.
+ * Q, out: the tokens of all sequences one after another, [sum of n_tokens][n_q_heads][64] bf16, where
+ * n_q_heads is a multiple g of the pool's n_heads and query head j attends to head j / g;
+ * K, V: [sum of n_tokens][n_heads][64] bf16.  lse: for each i in turn [n_q_heads][n_tokens[i]] fp32,
+ * natural log.  A query without any key gets out 0 and lse -infinity.  Pages that neighbours in
+ * `seqs` have in common are read once for the queries of all of them where that saves work: name forks of one
+ * sequence next to each other.  A sequence may be named more than once.
+ * n_tokens[i] in [0, 16384].  Arithmetic as rv_attend_frame; results do not depend on what else is in the
+ * batch beyond its rounding.  Allocates nothing and does not synchronise. */
+rv_status rv_attend_seqs(rv_pool p, int n, const int *seqs, const int *n_tokens, const void *Q, const void *K,
+                         const void *V, int n_q_heads, void *out, float *lse, void *stream);
+
+/* rv_admit_layers for frames of n sequences (Sec. 3.3, Eq. 6): the saliency of each frame's keys from
+ * its queries and the LSE of rv_attend_seqs, then per head the `budget` most salient rows, appended to
+ * the sequence in ascending token order.  Q, K, V: [n][n_tokens][n_heads][64] bf16 (as many query heads as
+ * heads); lse, saliency_out: [n][n_heads][n_tokens] fp32; idx_out: [n][n_heads][budget] int32; all required.
+ * A sequence may be named once.  n <= 4096. */
+rv_status rv_admit_seqs(rv_pool p, int n, const int *seqs, const void *Q, const void *K, const void *V,
+                        const float *lse, int n_tokens, const rv_qsub *qs, int budget, float *saliency_out,
+                        int32_t *idx_out, void *stream);
+
 /* Synchronises the current device and reports any error the HIP runtime recorded for
  * earlier work (RV_ERR_HIP with the runtime's message).  Test harnesses call it after
  * each step. */

@@ -10,6 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librv.so")
 SYNTH_LIB = os.path.join(HERE, "librv_synth.so")
 BIND_LIB = os.path.join(HERE, "_rv_bind.so")
+SOURCES = ("rv_host.cpp", "rv_plan.cpp", "rv_prepare.cpp", "rv_pool.cpp", "rv_seq.cpp", "attend.hip", "admit.hip",
+           "prepare.hip", "pages.hip", "attend_seqs.hip")
 ARCH = os.environ.get("RV_OFFLOAD_ARCH", "gfx950")
 
 HIPCC_FLAGS = [
@@ -46,8 +48,7 @@ def _build_bind(verbose):
 
 
 def build(verbose: bool = False):
-    _hipcc(LIB, [os.path.join(CSRC, f) for f in ("rv_host.cpp", "rv_plan.cpp", "attend.hip", "admit.hip")], verbose,
-           KERNEL_FLAGS)
+    _hipcc(LIB, [os.path.join(CSRC, f) for f in SOURCES], verbose, KERNEL_FLAGS)
     _hipcc(SYNTH_LIB, [os.path.join(CSRC, "synth_gpu.hip")], verbose)
     _build_bind(verbose)
     return LIB, SYNTH_LIB

@@ -681,6 +681,7 @@ __global__ __launch_bounds__(NT) void select_kernel(AdmitArgs a) {
     const int h = h_own;
     if (L.idx)
       for (int r = tid; r < k; r += NT) L.idx[(int64_t)h * k + r] = s_idx[r];
+    if (!L.memK) return;  // the caller appends the rows
     // 16-byte chunks: 8 per K row, 8 per V row.
     if (!a.in_place) {
       for (int c = tid; c < k * 16; c += NT) {

@@ -1,0 +1,137 @@
+// pages.hip -- rows into, out of and within the pages of a pool, gfx950.
+//
+// A page is 64 rows of every head, [H][64][64] bf16 for K and the same for V; a sequence's pages are
+// listed in its row of the device's page table.  All kernels here move 16-byte chunks, eight lanes to a
+// row's 128 bytes, so that every access is whole cache lines whatever rows are picked; they are
+// bound by memory.  A workgroup finds its sequence by its first-block number.
+#include "rv_internal.h"
+#include "rv_ops.h"
+
+namespace rv {
+namespace {
+
+constexpr int D = kHeadDim;
+constexpr int NT = 256;
+constexpr int kRowsPerBlock = NT / 8;
+static_assert(kRowsPerBlock == kPageBlockRows, "the host counts workgroups by it");
+
+// The last i < n whose block0 is at or below the workgroup's number (block0 ascends).
+template <class S>
+__device__ __forceinline__ int my_seq(const S* seq, int n) {
+  const int lane = threadIdx.x & 63;
+  int count = 0;
+  for (int i = 0; i < n; i += 64)
+    count += __popcll(__ballot(i + lane < n && seq[min(i + lane, n - 1)].block0 <= (int)blockIdx.x));
+  return __builtin_amdgcn_readfirstlane(count - 1);
+}
+
+__device__ __forceinline__ int64_t page_at(int page, int H, int h, int row) {
+  return (((int64_t)page * H + h) * kPageRows + row) * D;
+}
+
+__global__ __launch_bounds__(64) void table_kernel(TableArgs a) {
+  const TableRun& r = a.run[blockIdx.x];
+  for (int i = threadIdx.x; i < r.count; i += 64)
+    a.table[r.dst + i] = r.copy ? a.table[r.src + i] : r.src + i;
+}
+
+// Frame rows [n][H][64] (or the picked ones of each head) to the sequences' pages.  Row i of a
+// sequence, i < offset, is a row before `start` in its first page: copied where that page is copied.
+__global__ __launch_bounds__(NT) void append_kernel(AppendArgs a) {
+  const AppendSeq& s = a.seq[my_seq(a.seq, a.n_seqs)];
+  const int H = a.n_heads, block = (int)blockIdx.x - s.block0;
+  if (block == 0 && threadIdx.x < 2 && (s.fresh >> threadIdx.x & 1)) a.table[s.entry0 + threadIdx.x] = s.page[threadIdx.x];
+  const int64_t r = (int64_t)block * kRowsPerBlock + (threadIdx.x >> 3);
+  const int e = 8 * (threadIdx.x & 7);
+  const int skip = s.cow >= 0 ? 0 : s.offset;  // rows of the first page that stay
+  const int64_t rows = (int64_t)(s.offset + s.n - skip) * H;
+  if (r >= rows) return;
+  const int i = skip + (int)(r / H), h = (int)(r % H), p = i / kPageRows;
+  const int page = p < 2 ? s.page[p] : a.table[s.entry0 + p];
+  const int64_t to = page_at(page, H, h, i % kPageRows) + e;
+  uint4 k, v;
+  if (i < s.offset) {
+    const int64_t from = page_at(s.cow, H, h, i) + e;
+    k = *reinterpret_cast<const uint4*>(a.K + from);
+    v = *reinterpret_cast<const uint4*>(a.V + from);
+  } else {
+    const int j = i - s.offset;
+    int64_t row = (int64_t)s.src_row + j;
+    if (a.idx) {
+      const int pick = a.idx[(int64_t)s.src_row * H + (int64_t)h * s.n + j];
+      row = (int64_t)(s.src_row / s.n) * a.idx_tokens + min(max(pick, 0), a.idx_tokens - 1);
+    }
+    const int64_t from = (row * H + h) * D + e;
+    k = *reinterpret_cast<const uint4*>(a.srcK + from);
+    v = *reinterpret_cast<const uint4*>(a.srcV + from);
+  }
+  *reinterpret_cast<uint4*>(a.K + to) = k;
+  *reinterpret_cast<uint4*>(a.V + to) = v;
+}
+
+// Rows of sequences to [H][n][64] blocks.
+__global__ __launch_bounds__(NT) void gather_kernel(GatherArgs a) {
+  const GatherSeq& s = a.seq[my_seq(a.seq, a.n_seqs)];
+  const int H = a.n_heads;
+  const int64_t r = (int64_t)((int)blockIdx.x - s.block0) * kRowsPerBlock + (threadIdx.x >> 3);
+  const int e = 8 * (threadIdx.x & 7);
+  if (r >= (int64_t)s.n * H) return;
+  const int h = (int)(r / s.n), i = s.offset + (int)(r - (int64_t)h * s.n);
+  const int64_t from = page_at(a.table[s.entry0 + i / kPageRows], H, h, i % kPageRows) + e;
+  const int64_t to = (s.dst_row + r) * D + e;
+  if (a.dstK) *reinterpret_cast<uint4*>(a.dstK + to) = *reinterpret_cast<const uint4*>(a.K + from);
+  if (a.dstV) *reinterpret_cast<uint4*>(a.dstV + to) = *reinterpret_cast<const uint4*>(a.V + from);
+}
+
+// The kept rows of a sequence to its new pages.
+__global__ __launch_bounds__(NT) void compact_kernel(CompactArgs a) {
+  const CompactSeq& s = a.seq[my_seq(a.seq, a.n_seqs)];
+  const int H = a.n_heads;
+  const int64_t r = (int64_t)((int)blockIdx.x - s.block0) * kRowsPerBlock + (threadIdx.x >> 3);
+  const int e = 8 * (threadIdx.x & 7);
+  const int per_head = s.offset + s.n;
+  if (r >= (int64_t)per_head * H) return;
+  const int h = (int)(r / per_head), i = (int)(r - (int64_t)h * per_head);
+  int row = s.base + i;
+  if (i >= s.offset) {
+    row = a.keep[s.keep0 + (int64_t)h * s.n + (i - s.offset)];
+    if (row < s.lo || row >= s.hi) row = -1;
+  }
+  uint4 k = make_uint4(0, 0, 0, 0), v = k;
+  if (row >= 0) {
+    const int64_t from = page_at(a.table[s.old0 + row / kPageRows], H, h, row % kPageRows) + e;
+    k = *reinterpret_cast<const uint4*>(a.K + from);
+    v = *reinterpret_cast<const uint4*>(a.V + from);
+  }
+  const int64_t to = page_at(a.table[s.new0 + i / kPageRows], H, h, i % kPageRows) + e;
+  *reinterpret_cast<uint4*>(a.K + to) = k;
+  *reinterpret_cast<uint4*>(a.V + to) = v;
+}
+
+}  // namespace
+
+hipError_t launch_table(const TableArgs& a, hipStream_t s) {
+  if (a.n == 0) return hipSuccess;
+  hipLaunchKernelGGL(table_kernel, dim3((unsigned)a.n), dim3(64), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_append(const AppendArgs& a, hipStream_t s) {
+  if (a.blocks == 0) return hipSuccess;
+  hipLaunchKernelGGL(append_kernel, dim3((unsigned)a.blocks), dim3(NT), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_gather(const GatherArgs& a, hipStream_t s) {
+  if (a.blocks == 0) return hipSuccess;
+  hipLaunchKernelGGL(gather_kernel, dim3((unsigned)a.blocks), dim3(NT), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_compact(const CompactArgs& a, hipStream_t s) {
+  if (a.blocks == 0) return hipSuccess;
+  hipLaunchKernelGGL(compact_kernel, dim3((unsigned)a.blocks), dim3(NT), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace rv

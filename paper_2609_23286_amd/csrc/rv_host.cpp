@@ -14,11 +14,12 @@
 #include <string>
 #include <vector>
 
-#include "rv_internal.h"
+#include "rv_host.h"
 
+namespace rv {
 namespace {
-
 thread_local std::string g_err;
+}
 
 rv_status fail(rv_status st, const char* fmt, ...) {
   char buf[512];
@@ -35,12 +36,13 @@ rv_status hip_fail(hipError_t e, const char* what) {
               hipGetErrorString(e));
 }
 
-#define RV_HIP(call, what)                       \
-  do {                                           \
-    hipError_t e_ = (call);                      \
-    if (e_ != hipSuccess) return hip_fail(e_, what); \
-  } while (0)
+const char* error_text() { return g_err.c_str(); }
+}  // namespace rv
 
+namespace {
+
+using rv::fail;
+using rv::hip_fail;
 
 // ---- per-device context: placement calibration, limits, scratch workspace --------
 //
@@ -59,6 +61,8 @@ struct Workspace {
   float* sal = nullptr;      // saliency staging when the caller passes none
   size_t sal_floats = 0;
   float* static_part = nullptr;  // this device's copy of the static partial-slot array
+  float* seq_part = nullptr;     // partial results of rv_attend_seqs (from the first rv_pool_create)
+  size_t seq_floats = 0;
 };
 
 std::mutex g_ws_mu;
@@ -149,16 +153,36 @@ rv_status check_qsub(const rv_qsub* qs, int n_tokens) {
 
 }  // namespace
 
-// ---- memory arena ----------------------------------------------------------------
-struct rv_mem_s {
-  int device = 0;
-  int n_heads = 0;
-  int64_t cap = 0, max_tokens = 0, len = 0;
-  uint16_t* K = nullptr;
-  uint16_t* V = nullptr;
-  int32_t* prov = nullptr;
-};
+namespace rv {
 
+rv_status device_context(DeviceContext* out) {
+  std::lock_guard<std::mutex> lk(g_ws_mu);
+  Workspace* ws;
+  rv_status st = ready_ws(&ws);
+  if (st != RV_OK) return st;
+  *out = DeviceContext{ws->n_cus, ws->n_queues, ws->max_lds, ws->part,
+                       (size_t)ws->part_slots * kAttnSlotFloats, ws->seq_part, ws->seq_floats};
+  return RV_OK;
+}
+
+rv_status check_current(int device, const char* what) {
+  int dev = 0;
+  RV_HIP(hipGetDevice(&dev), "hipGetDevice");
+  if (dev != device) return fail(RV_ERR_INVALID, "%s lives on device %d but device %d is current", what, device, dev);
+  return RV_OK;
+}
+
+rv_status setup_sequences() {
+  std::lock_guard<std::mutex> lk(g_ws_mu);
+  Workspace* ws;
+  rv_status st = setup_ws(&ws);
+  if (st != RV_OK) return st;
+  return grow_floats(&ws->seq_part, &ws->seq_floats, kSeqPartFloats, "sequence attention workspace");
+}
+
+}  // namespace rv
+
+// ---- memory arena ----------------------------------------------------------------
 namespace {
 
 // Arenas are stream-ordered allocations (hipMallocAsync / hipFreeAsync on the stream of
@@ -225,19 +249,13 @@ rv_status arena_reserve(rv_mem m, int64_t tokens, hipStream_t s) {
   return RV_OK;
 }
 
-rv_status check_device(rv_mem m) {
-  int dev = 0;
-  RV_HIP(hipGetDevice(&dev), "hipGetDevice");
-  if (dev != m->device)
-    return fail(RV_ERR_INVALID, "memory lives on device %d but device %d is current", m->device, dev);
-  return RV_OK;
-}
+rv_status check_device(rv_mem m) { return rv::check_current(m->device, "memory"); }
 
 }  // namespace
 
 extern "C" {
 
-const char* rv_last_error(void) { return g_err.c_str(); }
+const char* rv_last_error(void) { return rv::error_text(); }
 
 const char* rv_version(void) { return "librv 0.1 (gfx950)"; }
 

@@ -30,4 +30,19 @@ hipError_t launch_xcc_probe(int* ids, int n_blocks, hipStream_t s);
 // max_lds: the device's LDS limit per workgroup (bytes), for the kernel attribute.
 hipError_t launch_admit(const AdmitArgs& a, int max_lds, hipStream_t s);
 
+struct PrepArgs;
+struct TableArgs;
+struct AppendArgs;
+struct GatherArgs;
+struct CompactArgs;
+struct SeqArgs;
+// The projections' norms and rotation, or (back) their gradients and, if any of the weights' and
+// biases' is asked for, the sum of the workgroups' partial sums.
+hipError_t launch_prepare(const PrepArgs& a, bool f32, int axes, bool back, hipStream_t s);
+hipError_t launch_table(const TableArgs& a, hipStream_t s);
+hipError_t launch_append(const AppendArgs& a, hipStream_t s);
+hipError_t launch_gather(const GatherArgs& a, hipStream_t s);
+hipError_t launch_compact(const CompactArgs& a, hipStream_t s);
+hipError_t launch_attend_seqs(const SeqArgs& a, hipStream_t s);
+
 }  // namespace rv

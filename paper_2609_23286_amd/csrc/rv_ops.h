@@ -1,0 +1,237 @@
+// rv_ops.h -- argument blocks and host-side planning of the operators around a frame's
+// attention (not installed): the projection's norms and rotation, the page pool, and the
+// attention of several sequences over shared pages.  Plain C++ with no HIP dependency, as
+// rv_plan.h.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/rv.h"
+#include "rv_plan.h"
+
+namespace rv {
+
+// Workgroups of 256 threads a launch may have: a grid holds fewer than 2^32 threads.
+constexpr int kMaxGridBlocks = 1 << 23;
+
+// ---- projection outputs to frame tensors ------------------------------------------------
+
+constexpr int kMaxFreqs = kHeadDim / 2;
+constexpr int kPrepThreads = 256;
+constexpr int kPrepMaxTokens = 8;  // tokens a wave takes at a time
+
+// Source and gradient rows are [n_tokens] rows of `stride` elements, head h at column 64 h.
+struct PrepArgs {
+  const void *q, *k, *v;        // bf16 or fp32 (v may be NULL)
+  int64_t q_stride, k_stride, v_stride;
+  const int32_t* pos;           // [n_tokens][axes]
+  uint16_t *Q, *K, *V;          // [n][Hq][64]; row j of kv head h at K / V + j kv_row + h kv_head
+  int64_t kv_row, kv_head;
+  const float *qw, *qb, *kw, *kb;  // [64] or NULL
+  const uint16_t *dQ, *dK, *dV;    // backward: [n][H][64] (dV may be NULL)
+  void *dq, *dk, *dv;
+  int64_t dq_stride, dk_stride, dv_stride;
+  float* part;                     // backward: [blocks][4][64] weight and bias sums
+  float *dqw, *dqb, *dkw, *dkb;    // [64] or NULL
+  int n_tokens, n_q_heads, n_kv_heads;
+  int norm;
+  float eps;
+  int tokens_per_wave;
+  int blocks;
+  uint64_t freq[kMaxFreqs];     // turns a position, in 2^-64 turns
+};
+
+// The turns one position step rotates pair i of an axis block by, base^(-i / n_freqs) / (2 pi),
+// as a fraction of 2^64: the product with a position wraps modulo whole turns, so the phase of
+// any 32-bit position is exact to 2^-32 turns.
+void rotation_turns(double base, int n_freqs, uint64_t* out);
+
+// ---- page pool --------------------------------------------------------------------------
+
+constexpr int kPageRows = RV_PAGE_ROWS;
+static_assert(kPageRows == kAttnBK, "a page is one key tile of the attention");
+
+// A run of page-table entries: entry dst + i becomes page src + i, or (copy) entry src + i.
+struct TableRun {
+  int32_t dst, src, count, copy;
+};
+constexpr int kMaxRuns = 240;
+constexpr int kPageBlockRows = 32;  // rows (of one head) a workgroup of the row-moving kernels takes
+struct TableArgs {
+  int32_t* table;
+  int n;
+  TableRun run[kMaxRuns];
+};
+
+// Rows written to sequences: sequence i's rows start at `start`, `n` of them from row src_row of
+// the packed frame.  The first two pages they touch are given here (and entered into the table
+// where new); later ones were entered by an earlier launch.
+struct AppendSeq {
+  int32_t block0;     // its first workgroup
+  int32_t entry0;     // table entry of the page that holds row `start`
+  int32_t page[2];
+  int32_t fresh;      // bit i: page[i] is new, its entry is written here
+  int32_t cow;        // page whose rows before `start` are copied to page[0], or -1
+  int32_t offset;     // start % 64
+  int32_t n;
+  int32_t src_row;
+};
+constexpr int kMaxAppend = 64;
+struct AppendArgs {
+  uint16_t *K, *V;    // pages [n_pages][H][64][64]
+  int32_t* table;
+  const uint16_t *srcK, *srcV;  // row j of head h: src + (src_row + j) H 64 + h 64
+  const int32_t* idx;           // NULL, or per sequence [H][n]: row j of head h is frame token
+                                //   idx[h][j] (sequence i's block starts at H src_row)
+  int idx_tokens;               // ... of a frame of this many tokens, sequence i's at i idx_tokens
+  int n_heads, n_seqs, blocks;
+  AppendSeq seq[kMaxAppend];
+};
+
+// Rows copied out of sequences into [H][n][64] blocks.
+struct GatherSeq {
+  int32_t block0;
+  int32_t entry0;     // table entry of the page that holds row `first`
+  int32_t offset;     // first % 64
+  int32_t n;
+  int64_t dst_row;    // sum of H n over earlier sequences
+};
+constexpr int kMaxGather = 128;
+struct GatherArgs {
+  const uint16_t *K, *V;
+  const int32_t* table;
+  uint16_t *dstK, *dstV;  // either may be NULL
+  int n_heads, n_seqs, blocks;
+  GatherSeq seq[kMaxGather];
+};
+
+// Rows of sequences gathered into new pages: row i >= offset of head h comes from row
+// keep[h][i - offset] of the old table row, row i < offset (the rows kept in place at the head
+// of the first new page) from old row base + i.
+struct CompactSeq {
+  int32_t block0;
+  int32_t old0, new0;  // first entries of the old table row and of the first new page
+  int32_t base;        // row of the sequence that the first new page starts at
+  int32_t offset;
+  int32_t n;           // kept rows after `offset`
+  int32_t lo, hi;      // rows that `keep` may name: [lo, hi)
+  int64_t keep0;       // sum of H n over earlier sequences
+};
+constexpr int kMaxCompact = 64;
+struct CompactArgs {
+  uint16_t *K, *V;
+  const int32_t* table;
+  const int32_t* keep;
+  int n_heads, n_seqs, blocks;
+  CompactSeq seq[kMaxCompact];
+};
+
+// A kernel's arguments hold at most 4 KB.
+static_assert(sizeof(TableArgs) <= 4096 && sizeof(AppendArgs) <= 4096 && sizeof(GatherArgs) <= 4096 &&
+              sizeof(CompactArgs) <= 4096, "kernel arguments");
+
+// Which sequence holds which pages, on the host.  Every array is allocated by init(), so no later
+// call allocates.  Entries of sequence s lie at row(s) * width; a compaction builds the new list in
+// the sequence's other row, so that the old one stays readable on the device meanwhile.
+class PageBook {
+ public:
+  PageBook() = default;
+  ~PageBook();
+  PageBook(const PageBook&) = delete;
+  PageBook& operator=(const PageBook&) = delete;
+  bool init(int n_pages, int max_seqs, int width);  // false: no memory
+
+  int width() const { return width_; }
+  int max_seqs() const { return max_seqs_; }
+  int free_pages() const { return n_free_; }
+  bool is_open(int s) const { return s >= 0 && s < max_seqs_ && open_[s]; }
+  int64_t len(int s) const { return len_[s]; }
+  int pages(int s) const { return (int)((len_[s] + kPageRows - 1) / kPageRows); }
+  int32_t entry0(int s) const { return (2 * s + side_[s]) * width_; }
+  int32_t page(int s, int i) const { return table_[entry0(s) + i]; }
+  const int32_t* list(int s) const { return table_ + entry0(s); }
+  int users(int page) const { return refs_[page]; }
+  // True once for every sequence of a batch: begin_batch() first.
+  void begin_batch() { ++batch_; }
+  bool first_in_batch(int s);
+
+  int open();                             // a new, empty sequence, or -1
+  int can_open() const { return n_closed_; }
+  void close(int s);
+  void fork(int child, int s, int64_t n_rows);
+  void truncate(int s, int64_t n_rows);
+
+  // Pages that appending n rows takes, the copy of a shared last page included.
+  int append_pages(int s, int64_t n) const;
+  bool append_copies(int s, int64_t n) const;  // whether the last page is shared and has to be copied
+  // Gives s the pages of n more rows.  A page that was copied is dropped by release_dropped(), so
+  // that nothing of this batch is written to a page that it still reads.  Returns that page or -1.
+  int append(int s, int64_t n);
+  // Gives s a new list: its pages before row `first`, then new ones up to `n_rows` rows, in its
+  // other table row.  The old pages are dropped by release_dropped().
+  int compact_pages(int64_t first, int64_t n_rows) const;
+  void compact(int s, int64_t first, int64_t n_rows);
+  void release_dropped();
+
+ private:
+  int take();
+  void drop(int page) { if (--refs_[page] == 0) free_[n_free_++] = page; }
+  int n_pages_ = 0, max_seqs_ = 0, width_ = 0, n_free_ = 0, n_closed_ = 0, n_dropped_ = 0, n_moved_ = 0;
+  int64_t batch_ = 0;
+  int32_t *table_ = nullptr, *refs_ = nullptr, *free_ = nullptr, *closed_ = nullptr;
+  int32_t *dropped_ = nullptr;  // pages that appends copied
+  int32_t *moved_ = nullptr, *old_pages_ = nullptr;  // compacted sequences, and how many pages each had
+  int64_t *len_ = nullptr, *stamp_ = nullptr;
+  uint8_t *open_ = nullptr, *side_ = nullptr;
+};
+
+// ---- attention of several sequences ----------------------------------------------------
+
+// A pass: queries of consecutive tokens over a range of pages that all of them attend to (and,
+// for one sequence's own pass, the frame keys of its tokens).  Passes form a forest: a sequence's
+// context is its own pass (a leaf) and the passes above it.
+struct SeqPass {
+  int32_t block0;     // first workgroup
+  int32_t tok0, n_tok;
+  int32_t entry0;     // table entry of the first page
+  int32_t n_pages;
+  int32_t last_rows;  // valid rows of the last page
+  int32_t frame;      // frame keys: n_tok or 0
+  int32_t parent;     // pass above, or -1
+  int32_t pieces;     // the key tiles are cut into this many pieces
+  int32_t q_tiles;    // query tiles of tile_rows rows
+  int32_t tile_rows;  // 128, or 32 where the pass has few queries
+  int32_t slot0;      // first partial slot (of 32 rows); -1: outputs are written directly
+  int32_t merge0;     // leaves: first workgroup of the merge launch
+};
+constexpr int kMaxPasses = 72;
+constexpr int kSubRows = 32;  // rows of a partial slot of this launch
+constexpr int kSubFloats = kSubRows * kHeadDim / 2 + 2 * kSubRows;
+struct SeqArgs {
+  const uint16_t *Q, *K, *V;      // packed frames [tokens][Hq or H][64]; K, V NULL without frame keys
+  const uint16_t *pageK, *pageV;  // [n_pages][H][64][64]
+  const int32_t* table;
+  uint16_t* out;
+  float* lse;
+  float* part;
+  int n_heads, group;             // kv heads, query heads to each
+  int n_pass, n_inner;            // passes; the first n_inner are not leaves
+  int blocks, merge_blocks;
+  SeqPass pass[kMaxPasses];
+};
+static_assert(sizeof(SeqArgs) <= 4096, "kernel arguments");
+
+struct SeqSpan {  // one sequence of a batch, as the plan sees it
+  int seq;
+  int n_tok;
+};
+
+// Plans one launch for sequences [0, n) of a batch (tokens packed in order, the first at tok0):
+// fills a's passes, returns how many of the sequences it covers (>= 1).
+int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool frame, int n_heads, int group,
+              int n_cus, int64_t max_slots, SeqArgs* a);
+
+inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+}  // namespace rv

@@ -107,7 +107,7 @@ struct AdmitLayer {
                            //   ([H][sal_tiles][N] per-block rows when sal_tiles > 0)
   float* sal_out;          // [H][N]       the summed saliency (sal_tiles > 0; optional)
   int32_t* idx;            // [H][budget]  optional output
-  uint16_t* memK;          // [H][head_stride][64]
+  uint16_t* memK;          // [H][head_stride][64]; NULL: the selection only goes to idx
   uint16_t* memV;
   int32_t* prov;           // [H][head_stride][2]
   int64_t mem_len;

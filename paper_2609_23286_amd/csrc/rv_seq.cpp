@@ -1,0 +1,295 @@
+// rv_seq.cpp -- host-side planning of the operators around a frame's attention: rotation
+// frequencies, the page pool's bookkeeping and the passes of an attention over several
+// sequences.  No device calls here, so this file also builds with a host compiler alone.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include "rv_ops.h"
+
+namespace rv {
+
+void rotation_turns(double base, int n_freqs, uint64_t* out) {
+  const long double two_pi = 6.283185307179586476925286766559005768L;
+  for (int i = 0; i < kMaxFreqs; ++i) {
+    out[i] = 0;
+    if (i >= n_freqs) continue;
+    const long double turns = powl((long double)base, -(long double)i / n_freqs) / two_pi;  // <= 0.16
+    out[i] = (uint64_t)(turns * 18446744073709551616.0L + 0.5L);
+  }
+}
+
+// ---- page pool --------------------------------------------------------------------------
+
+namespace {
+template <class T>
+bool alloc(T** p, int64_t n) {
+  *p = new (std::nothrow) T[(size_t)std::max<int64_t>(n, 1)]();
+  return *p != nullptr;
+}
+}  // namespace
+
+PageBook::~PageBook() {
+  delete[] table_;
+  delete[] refs_;
+  delete[] free_;
+  delete[] closed_;
+  delete[] dropped_;
+  delete[] moved_;
+  delete[] old_pages_;
+  delete[] len_;
+  delete[] stamp_;
+  delete[] open_;
+  delete[] side_;
+}
+
+bool PageBook::init(int n_pages, int max_seqs, int width) {
+  n_pages_ = n_pages;
+  max_seqs_ = max_seqs;
+  width_ = width;
+  const bool ok = alloc(&table_, 2 * (int64_t)max_seqs * width) && alloc(&refs_, n_pages) && alloc(&free_, n_pages) &&
+                  alloc(&closed_, max_seqs) && alloc(&dropped_, max_seqs) && alloc(&moved_, max_seqs) &&
+                  alloc(&old_pages_, max_seqs) && alloc(&len_, max_seqs) && alloc(&stamp_, max_seqs) &&
+                  alloc(&open_, max_seqs) && alloc(&side_, max_seqs);
+  if (!ok) return false;
+  // the lowest page and the lowest sequence go first
+  for (int i = 0; i < n_pages; ++i) free_[i] = n_pages - 1 - i;
+  for (int i = 0; i < max_seqs; ++i) closed_[i] = max_seqs - 1 - i;
+  n_free_ = n_pages;
+  n_closed_ = max_seqs;
+  return true;
+}
+
+bool PageBook::first_in_batch(int s) {
+  if (stamp_[s] == batch_) return false;
+  stamp_[s] = batch_;
+  return true;
+}
+
+int PageBook::take() {
+  const int p = free_[--n_free_];
+  refs_[p] = 1;
+  return p;
+}
+
+int PageBook::open() {
+  if (n_closed_ == 0) return -1;
+  const int s = closed_[--n_closed_];
+  open_[s] = 1;
+  len_[s] = 0;
+  return s;
+}
+
+void PageBook::close(int s) {
+  truncate(s, 0);
+  open_[s] = 0;
+  closed_[n_closed_++] = s;
+}
+
+void PageBook::fork(int child, int s, int64_t n_rows) {
+  len_[child] = n_rows;
+  const int n = pages(child);
+  const int32_t from = entry0(s), to = entry0(child);
+  for (int i = 0; i < n; ++i) {
+    table_[to + i] = table_[from + i];
+    ++refs_[table_[from + i]];
+  }
+}
+
+void PageBook::truncate(int s, int64_t n_rows) {
+  const int have = pages(s);
+  len_[s] = n_rows;
+  for (int i = pages(s); i < have; ++i) drop(page(s, i));
+}
+
+bool PageBook::append_copies(int s, int64_t n) const {
+  return n > 0 && len_[s] % kPageRows != 0 && refs_[page(s, pages(s) - 1)] > 1;
+}
+
+int PageBook::append_pages(int s, int64_t n) const {
+  return (int)(ceil_div64(len_[s] + n, kPageRows) - pages(s)) + (append_copies(s, n) ? 1 : 0);
+}
+
+int PageBook::append(int s, int64_t n) {
+  const int have = pages(s);
+  const bool copies = append_copies(s, n);
+  len_[s] += n;
+  int old = -1;
+  if (copies) {
+    old = page(s, have - 1);
+    dropped_[n_dropped_++] = old;
+    table_[entry0(s) + have - 1] = take();
+  }
+  for (int i = have; i < pages(s); ++i) table_[entry0(s) + i] = take();
+  return old;
+}
+
+int PageBook::compact_pages(int64_t first, int64_t n_rows) const {
+  return (int)(ceil_div64(n_rows, kPageRows) - first / kPageRows);
+}
+
+void PageBook::compact(int s, int64_t first, int64_t n_rows) {
+  const int keep = (int)(first / kPageRows);
+  moved_[n_moved_++] = s;
+  old_pages_[s] = pages(s);
+  const int32_t from = entry0(s);
+  side_[s] ^= 1;
+  len_[s] = n_rows;
+  const int32_t to = entry0(s);
+  for (int i = 0; i < keep; ++i) {
+    table_[to + i] = table_[from + i];
+    ++refs_[table_[from + i]];
+  }
+  for (int i = keep; i < pages(s); ++i) table_[to + i] = take();
+}
+
+void PageBook::release_dropped() {
+  while (n_dropped_ > 0) drop(dropped_[--n_dropped_]);
+  while (n_moved_ > 0) {
+    const int s = moved_[--n_moved_];
+    const int32_t old = (2 * s + (side_[s] ^ 1)) * width_;
+    for (int i = 0; i < old_pages_[s]; ++i) drop(table_[old + i]);
+  }
+}
+
+// ---- attention of several sequences ----------------------------------------------------
+
+namespace {
+
+// Full pages that sequences a and b have in common from their start.
+int common_pages(const PageBook& book, int a, int b) {
+  const int n = (int)(std::min(book.len(a), book.len(b)) / kPageRows);
+  if (n == 0) return 0;
+  const int32_t *x = book.list(a), *y = book.list(b);
+  constexpr int kStep = 128;
+  int i = 0;
+  while (i + kStep <= n && memcmp(x + i, y + i, kStep * sizeof(int32_t)) == 0) i += kStep;
+  while (i < n && x[i] == y[i]) ++i;
+  return i;
+}
+
+struct Builder {
+  const PageBook& book;
+  const SeqSpan* spans;
+  const int* tok;      // tokens before sequence i
+  const int* common;   // pages in common of sequences i and i + 1
+  int n_heads, group;
+  bool frame;
+  SeqArgs* a;
+  SeqPass leaf[kMaxPasses];
+  int n_leaf, n_inner;
+  bool overflow;
+
+  int64_t tiles(int64_t n_tok) const { return ceil_div64(n_tok * group, tile_rows(n_tok)); }
+  int tile_rows(int64_t) const { return kAttnBQ; }
+
+  SeqPass make(int i, int j, int p0, int p1, int parent) const {
+    SeqPass p{};
+    p.tok0 = tok[i];
+    p.n_tok = tok[j] - tok[i];
+    p.entry0 = book.entry0(spans[i].seq) + p0;
+    p.n_pages = p1 - p0;
+    p.last_rows = kPageRows;
+    p.parent = parent;
+    p.tile_rows = tile_rows(p.n_tok);
+    p.q_tiles = (int)tiles(p.n_tok);
+    return p;
+  }
+
+  // Sequences [i, j), whose first p0 pages the passes above cover.
+  void build(int i, int j, int p0, int parent) {
+    if (overflow) return;
+    if (j - i == 1) {
+      if (n_leaf + n_inner >= kMaxPasses) {
+        overflow = true;
+        return;
+      }
+      const int s = spans[i].seq;
+      SeqPass p = make(i, j, p0, book.pages(s), parent);
+      if (p.n_pages > 0) p.last_rows = (int)(book.len(s) - (int64_t)(book.pages(s) - 1) * kPageRows);
+      p.frame = frame ? p.n_tok : 0;
+      leaf[n_leaf++] = p;
+      return;
+    }
+    int shared = common[i];
+    for (int k = i + 1; k + 1 < j; ++k) shared = std::min(shared, common[k]);
+    int64_t apart = 0;
+    for (int k = i; k < j; ++k) apart += tiles(spans[k].n_tok);
+    const int64_t saved = (apart - tiles(tok[j] - tok[i])) * (shared - p0);
+    if (saved > 0) {
+      if (n_leaf + n_inner >= kMaxPasses) {
+        overflow = true;
+        return;
+      }
+      a->pass[n_inner] = make(i, j, p0, shared, parent);
+      parent = n_inner++;
+      p0 = shared;
+    } else if (shared > p0) {  // not worth a pass: every sequence takes these pages by itself
+      for (int k = i; k < j; ++k) build(k, k + 1, p0, parent);
+      return;
+    }
+    for (int k = i; k < j;) {
+      int e = k + 1;
+      while (e < j && common[e - 1] > p0) ++e;
+      build(k, e, p0, parent);
+      k = e;
+    }
+  }
+};
+
+}  // namespace
+
+int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool frame, int n_heads, int group,
+              int n_cus, int64_t max_slots, SeqArgs* a) {
+  n = std::min(n, kMaxPasses - 1);
+  int tok[kMaxPasses + 1], common[kMaxPasses] = {};
+  tok[0] = tok0;
+  for (int i = 0; i < n; ++i) tok[i + 1] = tok[i] + spans[i].n_tok;
+  for (int i = 0; i + 1 < n; ++i) common[i] = common_pages(book, spans[i].seq, spans[i + 1].seq);
+  for (;; n = (n + 1) / 2) {
+    Builder b{book, spans, tok, common, n_heads, group, frame, a, {}, 0, 0, false};
+    for (int k = 0; k < n;) {
+      int e = k + 1;
+      while (e < n && common[e - 1] > 0) ++e;
+      b.build(k, e, 0, -1);
+      k = e;
+    }
+    if (b.overflow) continue;
+    a->n_inner = b.n_inner;
+    a->n_pass = b.n_inner + b.n_leaf;
+    std::copy(b.leaf, b.leaf + b.n_leaf, a->pass + b.n_inner);
+    int64_t work = 0;
+    auto key_tiles = [](const SeqPass& p) { return p.n_pages + (int)ceil_div64(p.frame, kPageRows); };
+    for (int i = 0; i < a->n_pass; ++i) work += (int64_t)a->pass[i].q_tiles * key_tiles(a->pass[i]) * n_heads;
+    // Pieces of about the same length, so many that the device's workgroup slots are filled.
+    constexpr int kMinTiles = 4;
+    int64_t e = std::max<int64_t>(kMinTiles, ceil_div64(work, (int64_t)kAttnWgPerCu * n_cus));
+    int64_t slots = 0;
+    for (;; e *= 2) {
+      int64_t blocks = 0, merge = 0;
+      slots = 0;
+      int most = 0;
+      for (int i = 0; i < a->n_pass; ++i) {
+        SeqPass& p = a->pass[i];
+        const bool is_leaf = i >= a->n_inner;
+        p.pieces = (int)std::max<int64_t>(1, ceil_div64(key_tiles(p), e));
+        const bool direct = is_leaf && p.parent < 0 && p.pieces == 1 && key_tiles(p) > 0;
+        if (key_tiles(p) == 0) p.pieces = 0;
+        most = std::max(most, p.pieces);
+        p.block0 = (int)blocks;
+        blocks += (int64_t)p.pieces * p.q_tiles * n_heads;
+        p.slot0 = direct ? -1 : (int)slots;
+        if (!direct) slots += (int64_t)p.pieces * p.q_tiles * n_heads * (p.tile_rows / kSubRows);
+        p.merge0 = (int)merge;
+        if (is_leaf && !direct) merge += ceil_div64((int64_t)p.n_tok * group, kSubRows) * n_heads;
+      }
+      a->blocks = (int)blocks;
+      a->merge_blocks = (int)merge;
+      if (slots <= max_slots || most <= 1) break;
+    }
+    if (slots <= max_slots || n == 1) return n;
+  }
+}
+
+}  // namespace rv

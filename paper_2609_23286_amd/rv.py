@@ -36,6 +36,12 @@ class rv_qsub(ctypes.Structure):
                 ("n_special", ctypes.c_int32), ("stride", ctypes.c_int32)]
 
 
+class rv_qkv_prep(ctypes.Structure):
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("n_axes", ctypes.c_int32), ("eps", ctypes.c_float), ("base", ctypes.c_double)] + [
+        (n, ctypes.c_void_p) for n in ("q_weight", "q_bias", "k_weight", "k_bias")]
+
+
 class rv_attn_plan(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_units", "q_tiles", "T", "U", "E", "E1", "n_first",
                                                "n_queues", "grid", "total_chunks")] + [
@@ -84,6 +90,23 @@ def _load():
         "rv_attention_plan": ([i32, i32, i64, i32, i32, i32, P(rv_attn_plan)], i32),
         "rv_attention_plan_long": ([P(rv_attn_plan)], i32),
         "rv_device_status": ([], i32),
+        "rv_prepare_qkv": ([P(rv_qkv_prep), vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, vp, vp, vp], i32),
+        "rv_mem_stage_qkv": ([vp, P(rv_qkv_prep), vp, i64, vp, i64, vp, i64, i32, i32, vp, vp, vp], i32),
+        "rv_prepare_qkv_bwd": ([P(rv_qkv_prep), vp, i64, vp, i64, i32, i32, vp, vp, vp, vp, vp, i64, vp, i64, vp, i64,
+                                vp, vp, vp, vp, vp], i32),
+        "rv_pool_create": ([i32, i32, i32, i32, i64, P(vp)], i32),
+        "rv_pool_destroy": ([vp], i32),
+        "rv_pool_free_pages": ([vp], i32),
+        "rv_pool_open": ([vp, P(i32)], i32),
+        "rv_pool_len": ([vp, i32], i64),
+        "rv_pool_fork": ([vp, i32, i64, i32, vp, vp], i32),
+        "rv_pool_close": ([vp, i32, vp], i32),
+        "rv_pool_truncate": ([vp, i32, i64], i32),
+        "rv_pool_append": ([vp, i32, vp, vp, vp, vp, vp], i32),
+        "rv_pool_gather": ([vp, i32, vp, vp, vp, vp, vp, vp], i32),
+        "rv_pool_compact": ([vp, i32, vp, vp, vp, vp, vp], i32),
+        "rv_attend_seqs": ([vp, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp], i32),
+        "rv_admit_seqs": ([vp, i32, vp, vp, vp, vp, vp, i32, P(rv_qsub), i32, vp, vp, vp], i32),
     }
     for name, (args, res) in sigs.items():
         f = getattr(lib, name)
@@ -425,6 +448,235 @@ def stage_frames(mems, K, V, stream=None):
     _check(_lib.rv_mem_stage_frames(L, arr(*[m.handle for m in mems]),
                                     _ptrs(K, L, shp, 2, "K"), _ptrs(V, L, shp, 2, "V"), N,
                                     _stream(stream)))
+
+# ---- a layer's projections to frame tensors ----------------------------------------
+
+RV_BF16, RV_F32 = range(2)
+_NORMS = {None: 0, "rms": 1, "layer": 2}
+
+
+class QKVPrep:
+    """What rv_prepare_qkv does to a layer's projections (rv_qkv_prep): the norm of query and key
+    heads (None, "rms" or "layer") with fp32 [64] weights and biases (each may be None), and the
+    rotation by `axes` position axes (0: none) of frequency base `base`."""
+
+    def __init__(self, n_q_heads, n_kv_heads, norm="layer", eps=1e-5, axes=2, base=100.0, q_weight=None, q_bias=None,
+                 k_weight=None, k_bias=None):
+        if norm not in _NORMS:
+            raise ValueError(f"norm: {norm!r} is not one of None, 'rms', 'layer'")
+        self.vectors = (q_weight, q_bias, k_weight, k_bias)  # (kept alive: the struct holds addresses)
+        for t, name in zip(self.vectors, ("q_weight", "q_bias", "k_weight", "k_bias")):
+            if t is not None and t.dtype != torch.float32:
+                raise TypeError(f"{name}: dtype {t.dtype}, expected torch.float32")
+        ptrs = [_ptr(t, (HEAD_DIM,), 4, "weight or bias") for t in self.vectors]
+        self.c = rv_qkv_prep(n_q_heads, n_kv_heads, _NORMS[norm], axes, eps, base, *ptrs)
+        self.n_q_heads, self.n_kv_heads, self.axes = n_q_heads, n_kv_heads, axes
+
+
+def _rows(t, heads, what):
+    """(address, elements between rows, rv_dtype) of [N, heads * 64] or [N, heads, 64] rows at any
+    distance, or (None, 0, None)."""
+    if t is None:
+        return None, 0, None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what}: expected a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{what}: must be a device tensor")
+    n = t.shape[0] if t.dim() else 0
+    width = heads * HEAD_DIM
+    if tuple(t.shape) not in ((n, width), (n, heads, HEAD_DIM)):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(n, width)} or {(n, heads, HEAD_DIM)}")
+    if t.stride(-1) != 1 or (t.dim() == 3 and heads > 1 and t.stride(1) != HEAD_DIM):
+        raise ValueError(f"{what}: the elements of a row must be contiguous")
+    if t.dtype == torch.float32:
+        dtype = RV_F32
+    elif t.element_size() == 2 and t.dtype != torch.float16:
+        dtype = RV_BF16
+    else:
+        raise TypeError(f"{what}: dtype {t.dtype}, expected bfloat16 or float32")
+    return t.data_ptr(), t.stride(0) if n > 1 else width, dtype
+
+
+def _prep_rows(ts, n):
+    """_rows of several (tensor, heads, name), which must hold n rows of one dtype."""
+    out, dtype = [], None
+    for t, heads, what in ts:
+        p, stride, d = _rows(t, heads, what)
+        if t is not None:
+            if t.shape[0] != n:
+                raise ValueError(f"{what}: {t.shape[0]} rows, expected {n}")
+            if dtype not in (None, d):
+                raise TypeError(f"{what}: {t.dtype} beside another dtype")
+            dtype = d
+        out += [p, stride]
+    return out, dtype
+
+
+def _positions(prep, pos, n):
+    if prep.axes == 0:
+        return None
+    if pos is not None and pos.dtype != torch.int32:
+        raise TypeError(f"pos: dtype {pos.dtype}, expected torch.int32")
+    return _ptr(pos, (n,) if prep.axes == 1 and pos is not None and pos.dim() == 1 else (n, prep.axes), 4, "pos")
+
+
+def prepare_qkv(prep, q, k, v, pos, Q, K, V, stream=None):
+    """rv_prepare_qkv: q [N, Hq * 64], k, v [N, Hk * 64] (bf16 or fp32, rows at any distance) to the frame
+    tensors Q [N, Hq, 64], K, V [N, Hk, 64] bf16; pos [N, axes] int32.  v and V may be None."""
+    N, Hq, Hk = q.shape[0], prep.n_q_heads, prep.n_kv_heads
+    src, dtype = _prep_rows(((q, Hq, "q"), (k, Hk, "k"), (v, Hk, "v")), N)
+    _check(_lib.rv_prepare_qkv(ctypes.byref(prep.c), *src, dtype, N, _positions(prep, pos, N),
+                               _ptr(Q, (N, Hq, HEAD_DIM), 2, "Q"), _ptr(K, (N, Hk, HEAD_DIM), 2, "K"),
+                               _ptr(V, (N, Hk, HEAD_DIM), 2, "V"), _stream(stream)))
+
+
+def stage_qkv(prep, q, k, v, pos, Q, mem, stream=None):
+    """rv_mem_stage_qkv: prepare_qkv whose K and V become the frame staged in mem."""
+    N, Hq, Hk = q.shape[0], prep.n_q_heads, prep.n_kv_heads
+    src, dtype = _prep_rows(((q, Hq, "q"), (k, Hk, "k"), (v, Hk, "v")), N)
+    _check(_lib.rv_mem_stage_qkv(mem.handle, ctypes.byref(prep.c), *src, dtype, N, _positions(prep, pos, N),
+                                 _ptr(Q, (N, Hq, HEAD_DIM), 2, "Q"), _stream(stream)))
+
+
+def prepare_qkv_bwd(prep, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight=None, dq_bias=None, dk_weight=None,
+                    dk_bias=None, stream=None):
+    """rv_prepare_qkv_bwd: the gradients dq, dk, dv of prepare_qkv's inputs (their dtype, rows at any
+    distance) and, where given, of the weights and biases ([64] fp32, overwritten), from dQ [N, Hq, 64]
+    and dK, dV [N, Hk, 64] bf16.  dV and dv may be None."""
+    N, Hq, Hk = q.shape[0], prep.n_q_heads, prep.n_kv_heads
+    rows, dtype = _prep_rows(((q, Hq, "q"), (k, Hk, "k"), (dq, Hq, "dq"), (dk, Hk, "dk"), (dv, Hk, "dv")), N)
+    sums = []
+    for t, name in ((dq_weight, "dq_weight"), (dq_bias, "dq_bias"), (dk_weight, "dk_weight"), (dk_bias, "dk_bias")):
+        if t is not None and t.dtype != torch.float32:
+            raise TypeError(f"{name}: dtype {t.dtype}, expected torch.float32")
+        sums.append(_ptr(t, (HEAD_DIM,), 4, name))
+    _check(_lib.rv_prepare_qkv_bwd(ctypes.byref(prep.c), *rows[:4], dtype, N, _positions(prep, pos, N),
+                                   _ptr(dQ, (N, Hq, HEAD_DIM), 2, "dQ"), _ptr(dK, (N, Hk, HEAD_DIM), 2, "dK"),
+                                   _ptr(dV, (N, Hk, HEAD_DIM), 2, "dV"), *rows[4:], *sums, _stream(stream)))
+
+
+# ---- sequences in pages ----------------------------------------------------------------
+
+PAGE_ROWS = 64
+
+
+def _ints(values, n, what, ctype=ctypes.c_int):
+    if values is None:
+        return None
+    if len(values) != n:
+        raise ValueError(f"{what}: {len(values)} values for {n} sequences")
+    return (ctype * n)(*values)
+
+
+class Pool:
+    """Sequences of rows in pages of 64 rows, shared between forks (rv_pool).  Sequences are
+    numbers that open() and fork() give."""
+
+    def __init__(self, n_heads, n_pages, max_seqs, max_rows, head_dim=HEAD_DIM):
+        self.handle = None
+        h = ctypes.c_void_p()
+        _check(_lib.rv_pool_create(n_heads, head_dim, n_pages, max_seqs, max_rows, ctypes.byref(h)))
+        self.handle = h
+        self.n_heads = n_heads
+
+    def close(self):
+        if self.handle:
+            _lib.rv_pool_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    @property
+    def free_pages(self):
+        return _lib.rv_pool_free_pages(self.handle)
+
+    def open(self):
+        """rv_pool_open: a new, empty sequence."""
+        s = ctypes.c_int()
+        _check(_lib.rv_pool_open(self.handle, ctypes.byref(s)))
+        return s.value
+
+    def len(self, seq):
+        """Rows of a sequence; -1 if it is not open."""
+        return _lib.rv_pool_len(self.handle, seq)
+
+    def fork(self, seq, n_rows=None, n=1, stream=None):
+        """rv_pool_fork: a list of n new sequences that share the first n_rows rows (default: all)."""
+        out = (ctypes.c_int * n)()
+        rows = self.len(seq) if n_rows is None else n_rows
+        _check(_lib.rv_pool_fork(self.handle, seq, rows, n, out, _stream(stream)))
+        return list(out)
+
+    def release(self, seqs):
+        """rv_pool_close: close sequences; pages without another user are free."""
+        _check(_lib.rv_pool_close(self.handle, len(seqs), _ints(seqs, len(seqs), "seqs")))
+
+    def truncate(self, seq, n_rows):
+        """rv_pool_truncate: drop the newest rows (host-side only)."""
+        _check(_lib.rv_pool_truncate(self.handle, seq, n_rows))
+
+    def append(self, seqs, K, V, n_rows, stream=None):
+        """rv_pool_append: n_rows[i] rows of K, V [sum of n_rows, H, 64] to seqs[i]."""
+        n = len(seqs)
+        shp = (sum(n_rows), self.n_heads, HEAD_DIM)
+        _check(_lib.rv_pool_append(self.handle, n, _ints(seqs, n, "seqs"), _ptr(K, shp, 2, "K"), _ptr(V, shp, 2, "V"),
+                                   _ints(n_rows, n, "n_rows"), _stream(stream)))
+
+    def gather(self, seqs, K, V, n_rows, first=None, stream=None):
+        """rv_pool_gather: rows first[i] (default 0) .. + n_rows[i] of seqs[i] to the next [H, n_rows[i], 64] of K
+        and V (contiguous, sum of n_rows * H rows in all; either may be None)."""
+        n, size = len(seqs), sum(n_rows) * self.n_heads * HEAD_DIM
+        for t, what in ((K, "K"), (V, "V")):
+            if t is not None and t.numel() != size:
+                raise ValueError(f"{what}: {t.numel()} elements, expected {size}")
+        _check(_lib.rv_pool_gather(
+            self.handle, n, _ints(seqs, n, "seqs"), _ints(first, n, "first", ctypes.c_int64),
+            _ints(n_rows, n, "n_rows", ctypes.c_int64), K if K is None else _ptr(K, tuple(K.shape), 2, "K"),
+            V if V is None else _ptr(V, tuple(V.shape), 2, "V"), _stream(stream)))
+
+    def compact(self, seqs, keep, n_keep, first=None, stream=None):
+        """rv_pool_compact: seqs[i] keeps its rows before first[i] (default 0) and the n_keep[i] rows of each
+        head that keep (int32, [H, n_keep[i]] for each i in turn) names."""
+        n, size = len(seqs), sum(n_keep) * self.n_heads
+        if keep is not None and (keep.numel() != size or keep.dtype != torch.int32):
+            raise ValueError(f"keep: {keep.numel()} values of {keep.dtype}, expected {size} of torch.int32")
+        _check(_lib.rv_pool_compact(self.handle, n, _ints(seqs, n, "seqs"), _ints(first, n, "first", ctypes.c_int64),
+                                    _ints(n_keep, n, "n_keep", ctypes.c_int64),
+                                    keep if keep is None else _ptr(keep, tuple(keep.shape), 4, "keep"),
+                                    _stream(stream)))
+
+
+def attend_seqs(Q, K, V, pool, seqs, n_tokens, out, lse, stream=None):
+    """rv_attend_seqs: the queries of several sequences, Q, out [sum of n_tokens, Hq, 64] bf16, over the
+    sequences' rows and (unless None) their own keys K, V [sum of n_tokens, H, 64]; lse: fp32,
+    [Hq, n_tokens[i]] for each i in turn ([n, Hq, N] where all have N tokens)."""
+    n, total = len(seqs), sum(n_tokens)
+    Hq = Q.shape[1]
+    shp, kv = (total, Hq, HEAD_DIM), (total, pool.n_heads, HEAD_DIM)
+    if lse.numel() != total * Hq:
+        raise ValueError(f"lse: {lse.numel()} elements, expected {total * Hq}")
+    _check(_lib.rv_attend_seqs(pool.handle, n, _ints(seqs, n, "seqs"), _ints(n_tokens, n, "n_tokens"),
+                               _ptr(Q, shp, 2, "Q"), _ptr(K, kv, 2, "K"), _ptr(V, kv, 2, "V"), Hq,
+                               _ptr(out, shp, 2, "out"), _ptr(lse, tuple(lse.shape), 4, "lse"), _stream(stream)))
+
+
+def admit_seqs(Q, K, V, lse, qs, budget, pool, seqs, saliency_out, idx_out, stream=None):
+    """rv_admit_seqs: each frame's `budget` most salient rows per head to its sequence.  Q, K, V
+    [n, N, H, 64] bf16; lse, saliency_out [n, H, N] fp32; idx_out [n, H, budget] int32."""
+    n, N, H, d = Q.shape
+    if (n, H) != (len(seqs), pool.n_heads):
+        raise ValueError(f"Q: {n} frames of {H} heads for {len(seqs)} sequences of {pool.n_heads} heads")
+    shp = (n, N, H, d)
+    q = qs if isinstance(qs, rv_qsub) else rv_qsub(*qs)
+    _check(_lib.rv_admit_seqs(pool.handle, n, _ints(seqs, n, "seqs"), _ptr(Q, shp, 2, "Q"), _ptr(K, shp, 2, "K"),
+                              _ptr(V, shp, 2, "V"), _ptr(lse, (n, H, N), 4, "lse"), N, ctypes.byref(q), budget,
+                              _ptr(saliency_out, (n, H, N), 4, "saliency_out"),
+                              _ptr(idx_out, (n, H, budget), 4, "idx_out"), _stream(stream)))
+
 
 # ---- seeded stream generator on the GPU (benchmark inputs) -------------------------
 _synth = None

@@ -1,0 +1,255 @@
+// Host checks of the page lists and of the passes planned over them: random batches of forks,
+// appends, compactions, truncations and closings against a plain model of every sequence's rows,
+// with a page's contents written and read in the order the kernels may take; and for every plan,
+// that each query meets every key of its context exactly once and no two results share a slot.
+#include <algorithm>
+#include <cstdio>
+#include <cstdlib>
+#include <map>
+#include <random>
+#include <set>
+#include <vector>
+
+#include "../../paper_2609_23286_amd/csrc/rv_ops.h"
+
+namespace {
+int g_fail = 0;
+#define CHECK(c, ...)                                 \
+  do {                                                \
+    if (!(c) && ++g_fail < 20) {                      \
+      std::fprintf(stderr, "%s:%d: ", __FILE__, __LINE__); \
+      std::fprintf(stderr, __VA_ARGS__);              \
+      std::fprintf(stderr, "\n");                     \
+    }                                                 \
+  } while (0)
+
+using rv::PageBook;
+std::mt19937 rng(12345);
+int uniform(int lo, int hi) { return std::uniform_int_distribution<int>(lo, hi)(rng); }
+
+struct World {
+  PageBook book;
+  int n_pages, max_seqs;
+  int64_t max_rows;
+  std::vector<std::vector<int>> page;         // contents
+  std::map<int, std::vector<int>> rows;       // the model
+  int next = 1;
+
+  World(int pages, int seqs, int64_t max) : n_pages(pages), max_seqs(seqs), max_rows(max) {
+    CHECK(book.init(pages, seqs, (int)((max + 63) / 64)), "init");
+    page.assign(pages, std::vector<int>(64, 0));
+  }
+  std::vector<int> some(int most) {
+    std::vector<int> all;
+    for (auto& r : rows) all.push_back(r.first);
+    std::shuffle(all.begin(), all.end(), rng);
+    all.resize(std::min<size_t>(all.size(), uniform(0, most)));
+    return all;
+  }
+  void verify() {
+    std::vector<int> users(n_pages, 0);
+    for (auto& r : rows) {
+      CHECK(book.is_open(r.first) && book.len(r.first) == (int64_t)r.second.size(), "length of %d", r.first);
+      for (int i = 0; i < book.pages(r.first); ++i) ++users[book.page(r.first, i)];
+      for (size_t i = 0; i < r.second.size(); ++i)
+        CHECK(page[book.page(r.first, i / 64)][i % 64] == r.second[i], "sequence %d row %zu", r.first, i);
+    }
+    int free = 0;
+    for (int p = 0; p < n_pages; ++p) {
+      CHECK(book.users(p) == users[p], "page %d has %d users, not %d", p, book.users(p), users[p]);
+      free += users[p] == 0;
+    }
+    CHECK(free == book.free_pages(), "%d free pages, not %d", book.free_pages(), free);
+    CHECK(book.can_open() == max_seqs - (int)rows.size(), "sequences to open");
+  }
+  // All reads of a batch see the pages as they were, or as the batch writes them, in any order: reads
+  // are taken before and after the writes, and both must give the same.
+  void append(const std::vector<int>& seqs) {
+    std::vector<int> n;
+    int64_t need = 0;
+    for (int s : seqs) {
+      int r = uniform(0, 3) ? uniform(0, 70) : uniform(0, 300);
+      if (book.len(s) + r > max_rows) r = 0;
+      n.push_back(r);
+      need += book.append_pages(s, r);
+    }
+    if (need > book.free_pages()) return;
+    struct Copy { int from, to, n; };
+    std::vector<Copy> copies;
+    std::vector<std::pair<std::pair<int, int>, int>> writes;
+    for (size_t i = 0; i < seqs.size(); ++i) {
+      if (n[i] == 0) continue;
+      const int64_t start = book.len(seqs[i]);
+      const int before = book.free_pages(), want = book.append_pages(seqs[i], n[i]);
+      const int old = book.append(seqs[i], n[i]);
+      CHECK(before - book.free_pages() == want, "pages taken");
+      if (old >= 0) copies.push_back({old, book.page(seqs[i], start / 64), (int)(start % 64)});
+      for (int k = 0; k < n[i]; ++k) {
+        const int64_t r = start + k;
+        writes.push_back({{book.page(seqs[i], r / 64), (int)(r % 64)}, next});
+        rows[seqs[i]].push_back(next++);
+      }
+    }
+    auto old_pages = page;
+    std::set<std::pair<int, int>> written;
+    for (auto& w : writes) {
+      CHECK(written.insert(w.first).second, "a row written twice");
+      page[w.first.first][w.first.second] = w.second;
+    }
+    for (auto& c : copies)
+      for (int r = 0; r < c.n; ++r) {
+        CHECK(page[c.from][r] == old_pages[c.from][r], "a copied row is written in the same batch");
+        CHECK(written.insert({c.to, r}).second, "a copied row written twice");
+      }
+    for (auto& c : copies)
+      for (int r = 0; r < c.n; ++r) page[c.to][r] = old_pages[c.from][r];
+    book.release_dropped();
+  }
+  void compact(const std::vector<int>& seqs) {
+    std::vector<int64_t> first, keep;
+    int64_t need = 0;
+    for (int s : seqs) {
+      const int64_t len = book.len(s);
+      first.push_back(uniform(0, (int)len));
+      keep.push_back(len > first.back() ? uniform(1, (int)std::min<int64_t>(max_rows - first.back(), len)) : 0);
+      if (keep.back() > 0) need += book.compact_pages(first.back(), first.back() + keep.back());
+    }
+    if (need > book.free_pages()) return;
+    auto old_pages = page;
+    std::set<int> fresh;
+    for (size_t i = 0; i < seqs.size(); ++i) {
+      const int s = seqs[i];
+      if (keep[i] == 0) {
+        book.truncate(s, first[i]);
+        rows[s].resize(first[i]);
+        continue;
+      }
+      auto was = rows[s];
+      rows[s].resize(first[i]);
+      for (int64_t k = 0; k < keep[i]; ++k) rows[s].push_back(was[uniform((int)first[i], (int)was.size() - 1)]);
+      book.compact(s, first[i], first[i] + keep[i]);
+      for (int k = (int)(first[i] / 64); k < book.pages(s); ++k) {
+        CHECK(fresh.insert(book.page(s, k)).second, "a new page given twice");
+        for (int r = 0; r < 64 && k * 64 + r < (int)rows[s].size(); ++r) page[book.page(s, k)][r] = rows[s][k * 64 + r];
+      }
+    }
+    // no page that the batch wrote is one that some old list still reads
+    for (int p : fresh) CHECK(book.users(p) == 1, "a new page with %d users", book.users(p));
+    book.release_dropped();
+  }
+
+  void plan(bool frame, int n_heads, int group) {
+    std::vector<int> all = some(40);
+    std::sort(all.begin(), all.end());
+    if (uniform(0, 1) && !all.empty()) all.push_back(all[0]);
+    std::vector<rv::SeqSpan> span;
+    for (int s : all) span.push_back({s, uniform(0, 3) ? uniform(1, 4) : uniform(1, 700)});
+    int tok0 = uniform(0, 50);
+    const int64_t max_slots = uniform(0, 3) ? 16384 : 64;
+    for (size_t i = 0; i < span.size();) {
+      rv::SeqArgs a{};
+      const int done = rv::plan_seqs(book, &span[i], (int)(span.size() - i), tok0, frame, n_heads, group,
+                                     uniform(1, 300), max_slots, &a);
+      CHECK(done >= 1 && done <= (int)(span.size() - i), "sequences covered");
+      CHECK(a.n_pass <= rv::kMaxPasses && a.n_pass - a.n_inner == done, "passes");
+      std::vector<char> used(max_slots, 0);
+      int block = 0, merge = 0;
+      for (int k = 0; k < a.n_pass; ++k) {
+        const rv::SeqPass& p = a.pass[k];
+        const int tiles = p.n_pages + (p.frame + 63) / 64;
+        CHECK(p.block0 == block, "first workgroup");
+        CHECK((int64_t)p.q_tiles * p.tile_rows >= (int64_t)p.n_tok * group, "query tiles");
+        CHECK(p.pieces <= tiles && (p.pieces > 0) == (tiles > 0), "pieces");
+        CHECK(p.parent < a.n_inner && (k < a.n_inner ? p.parent < k : true), "parent");
+        block += p.pieces * p.q_tiles * n_heads;
+        if (p.slot0 >= 0) {
+          const int64_t n = (int64_t)p.pieces * p.q_tiles * n_heads * (p.tile_rows / rv::kSubRows);
+          CHECK(p.slot0 + n <= max_slots, "slots past the end");
+          for (int64_t s = p.slot0; s < p.slot0 + n && s < max_slots; ++s) CHECK(!used[s]++, "slot used twice");
+        } else {
+          CHECK(k >= a.n_inner && p.parent < 0 && p.pieces == 1, "a direct pass");
+        }
+        if (k >= a.n_inner) {
+          CHECK(p.merge0 == merge, "first merge workgroup");
+          if (p.slot0 >= 0) merge += (p.n_tok * group + rv::kSubRows - 1) / rv::kSubRows * n_heads;
+        }
+      }
+      CHECK(block == a.blocks && merge == a.merge_blocks, "workgroups");
+      for (int k = 0; k < done; ++k) {  // the pages from the leaf up are the sequence's, in order
+        const rv::SeqSpan& s = span[i + k];
+        const rv::SeqPass& leaf = a.pass[a.n_inner + k];
+        CHECK(leaf.tok0 == tok0 && leaf.n_tok == s.n_tok && leaf.frame == (frame ? s.n_tok : 0), "leaf");
+        int end = book.pages(s.seq);
+        if (leaf.n_pages > 0) CHECK(leaf.last_rows == book.len(s.seq) - (int64_t)(end - 1) * 64, "last rows");
+        for (int j = a.n_inner + k; j >= 0; j = a.pass[j].parent) {
+          const rv::SeqPass& p = a.pass[j];
+          CHECK(p.tok0 <= tok0 && tok0 + s.n_tok <= p.tok0 + p.n_tok, "tokens of a pass");
+          if (j < a.n_inner) CHECK(p.last_rows == 64, "a shared page is full");
+          end -= p.n_pages;
+          for (int q = 0; q < p.n_pages && end >= 0; ++q)
+            CHECK(book.list(s.seq)[end + q] == (book.list(0) - book.entry0(0))[p.entry0 + q], "page of a pass");
+        }
+        CHECK(end == 0, "pages covered");
+        tok0 += s.n_tok;
+      }
+      i += done;
+    }
+  }
+};
+
+void check_turns() {
+  uint64_t f[rv::kMaxFreqs];
+  rv::rotation_turns(1.0, 32, f);
+  // 2^64 / (2 pi) = 2.93589050328200122...e18
+  CHECK(f[0] >= 2935890503282001220ull && f[0] <= 2935890503282001232ull && f[31] == f[0], "turns %llu",
+        (unsigned long long)f[0]);
+  rv::rotation_turns(10000.0, 16, f);
+  CHECK(f[8] > f[0] / 100 - 2 && f[8] < f[0] / 100 + 2 && f[16] == 0, "turns of a lower frequency");
+}
+}  // namespace
+
+int main() {
+  check_turns();
+  for (int round = 0; round < 60; ++round) {
+    World w(uniform(1, 120), uniform(1, 24), uniform(0, 3) ? 1500 : uniform(1, 200));
+    for (int step = 0; step < 120; ++step) {
+      const int what = uniform(0, 9);
+      if (what <= 1) {
+        const int s = w.book.open();
+        CHECK((s < 0) == ((int)w.rows.size() == w.max_seqs), "open");
+        if (s >= 0) CHECK(w.rows.emplace(s, std::vector<int>()).second, "an open sequence given again");
+      } else if (what <= 3 && !w.rows.empty()) {
+        const int parent = std::next(w.rows.begin(), uniform(0, (int)w.rows.size() - 1))->first;
+        const auto was = w.rows[parent];
+        const int n = uniform(0, 3) ? (int)was.size() : uniform(0, (int)was.size());
+        for (int i = uniform(1, 4); i > 0 && w.book.can_open() > 0; --i) {
+          const int c = w.book.open();
+          w.book.fork(c, parent, n);
+          w.rows[c] = std::vector<int>(was.begin(), was.begin() + n);
+        }
+      } else if (what <= 6) {
+        w.append(w.some(6));
+      } else if (what == 7) {
+        w.compact(w.some(3));
+      } else if (what == 8) {
+        for (int s : w.some(1)) {
+          w.rows[s].resize(uniform(0, (int)w.rows[s].size()));
+          w.book.truncate(s, w.rows[s].size());
+        }
+      } else {
+        for (int s : w.some(2)) {
+          w.book.close(s);
+          w.rows.erase(s);
+        }
+      }
+      w.verify();
+      if (step % 10 == 9) w.plan(uniform(0, 1), uniform(1, 16), uniform(1, 4));
+    }
+  }
+  if (g_fail) {
+    std::fprintf(stderr, "%d checks failed\n", g_fail);
+    return 1;
+  }
+  std::printf("sequence logic OK\n");
+  return 0;
+}
