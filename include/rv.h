@@ -392,7 +392,7 @@ typedef struct rv_pool_s *rv_pool;
 
 /* A pool of n_pages pages for up to max_seqs open sequences of up to max_rows rows, on the current
  * device.  head_dim must be 64.  Runs rv_init and allocates everything later calls use, the
- * partial results of rv_attend_seqs among it (71 MB once per device).  Synchronous. */
+ * partial results of rv_attend_seqs among it (69 MB once per device).  Synchronous. */
 rv_status rv_pool_create(int n_heads, int head_dim, int n_pages, int max_seqs, int64_t max_rows, rv_pool *out);
 
 /* Frees the pool (synchronises its device first).  NULL is accepted. */

@@ -3,11 +3,11 @@
 // As attend.hip for one frame (z = q k / 8, LSE = log sum exp z, o = sum exp(z - LSE) v), with the
 // context of a query made of passes: a pass is a range of pages that a run of sequences has in
 // common, with the queries of all of them as one list of rows (token, query head of the group), so
-// that shared keys and values are read once for all.  A workgroup takes one query tile of one
-// kv head over one piece of a pass's key tiles; a page is one tile.  Softmax sums of disjoint key
-// sets combine exactly, so each piece writes its normalised output with its reference and row sum, and
-// the merge launch joins, per query, the pieces of its sequence's pass and of the passes above
-// it, in a fixed order.
+// that shared keys and values are read once for all.  The key tiles (a page is one) of all
+// units -- a query tile of one kv head of a pass -- are one list, cut into equal chunks, a workgroup
+// each.  Softmax sums of disjoint key sets combine exactly, so a segment of a unit writes its
+// sums with their reference, and the merge launch joins, per query, the segments of its sequence's
+// pass and of the passes above it, in a fixed order.
 #include <type_traits>
 
 #include "attn_tile.h"
@@ -30,13 +30,9 @@ struct SeqCursor {
   const char *pk, *pv;   // this head's rows of page 0
   const char *fk, *fv;   // this head's rows of the pass's first token
   int64_t page_bytes;    // bytes between pages
-  int64_t frame_bytes;   // bytes between frame tiles
   const int32_t* entry;  // the pass's table entries
-  int pages;             // this lane's entry: of tile base + lane
-  int base;
   int n_pages, n_tiles;
   int last_rows, frame_rows;  // valid rows of the last page and of the last frame tile
-  uint32_t r, g0, g1;    // this thread's row (and row + 32) of a tile, byte offsets in the rows
   uint32_t frame_row;    // bytes between frame rows
 
   __device__ __forceinline__ int valid(int t) const {
@@ -45,91 +41,308 @@ struct SeqCursor {
     if (t == n_pages - 1) v = last_rows;
     return v;
   }
-  __device__ __forceinline__ void fetch_entries(int t) {  // of tiles t .. t + 63
-    base = t;
-    pages = entry[min(t + (int)(threadIdx.x & 63), n_pages - 1)];
+};
+
+__device__ __forceinline__ const char* uniform_ptr(const char* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = (uint32_t)uniform((int)(uint32_t)x), hi = (uint32_t)uniform((int)(uint32_t)(x >> 32));
+  return reinterpret_cast<const char*>((uint64_t)hi << 32 | lo);
+}
+
+// Where a tile's rows lie (uniform).
+struct TileRows {
+  const char *k, *v;
+  uint32_t row;   // bytes between rows
+  uint32_t last;  // last valid row: rows past it are read as that one (pages hold anything there,
+                  // and a weight of zero makes zero only of numbers)
+};
+
+// The tiles a wave loads, in turn: index i is tile first + i step.  Their page numbers are held a lane
+// each and fetched 64 at a time, so that no tile's addresses wait for memory (a scalar load of the entry
+// for each tile cost a tenth of the forward launch).
+struct TileOrder {
+  int first, step;
+  int base = 0;   // index of lane 0's page
+  int pages;      // this lane's page number
+  __device__ __forceinline__ int at(int i) const { return first + i * step; }
+  __device__ __forceinline__ void fetch(const SeqCursor& tc, int i) {
+    base = i;
+    pages = tc.n_pages > 0 ? tc.entry[min(at(i + (int)(threadIdx.x & 63)), tc.n_pages - 1)] : 0;
   }
-  // Tile t's K and V into a ring stage (the wave's rows of it).  Rows past the tile's last valid one
-  // are read as that one: pages hold anything there, and their weights are zero only for numbers.
-  __device__ __forceinline__ void load(int t, uint16_t* st) {
-    const uint32_t last = (uint32_t)valid(t) - 1;
-    const char *k, *v;
-    uint32_t row;
-    if (t < n_pages) {
-      if (t - base >= 64) fetch_entries(t);
-      const int64_t at = (int64_t)__builtin_amdgcn_readlane(pages, t - base) * page_bytes;
-      k = pk + at;
-      v = pv + at;
-      row = D * 2;
+  __device__ __forceinline__ TileRows rows(const SeqCursor& tc, int i) {
+    const int t = at(i);
+    TileRows r;
+    r.last = (uint32_t)tc.valid(t) - 1;
+    if (t < tc.n_pages) {  // uniform
+      if (i - base >= 64) fetch(tc, i);
+      const int64_t at = (int64_t)__builtin_amdgcn_readlane(pages, i - base) * tc.page_bytes;
+      r.k = tc.pk + at;
+      r.v = tc.pv + at;
+      r.row = D * 2;
     } else {
-      const int64_t at = (t - n_pages) * frame_bytes;
-      k = fk + at;
-      v = fv + at;
-      row = frame_row;
+      const int64_t at = (int64_t)(t - tc.n_pages) * BK * tc.frame_row;
+      r.k = tc.fk + at;
+      r.v = tc.fv + at;
+      r.row = tc.frame_row;
     }
-    const uint32_t o0 = min(r, last) * row + g0, o1 = min(r + 32, last) * row + g1;
-    lds_load16(k + o0, st);
-    lds_load16(k + o1, st + 32 * D);
-    lds_load16(v + o0, st + TILE);
-    lds_load16(v + o1, st + TILE + 32 * D);
+    r.k = uniform_ptr(r.k);
+    r.v = uniform_ptr(r.v);
+    return r;
   }
 };
 
-__global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
-  __shared__ __attribute__((aligned(16))) uint16_t lds[NSTAGE * STAGE];
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
-  const int H = a.n_heads, G = a.group;
-  const int ip = last_at_or_below(0, a.n_pass, (int)blockIdx.x, [&](int i) { return a.pass[i].block0; });
-  const SeqPass& p = a.pass[ip];
-  // workgroups of a pass: head fastest, so that (the workgroups being dealt to the XCDs in turn) a
-  // head's query tiles share an L2; then query tiles; then pieces
-  const int b = (int)blockIdx.x - p.block0;
-  const int h = uniform(b % H), qt = uniform(b / H % p.q_tiles), piece = uniform(b / H / p.q_tiles);
-  const int n_tiles = p.n_pages + (p.frame + BK - 1) / BK;
-  const int t0 = uniform((int)((int64_t)piece * n_tiles / p.pieces));
-  const int t1 = uniform((int)((int64_t)(piece + 1) * n_tiles / p.pieces));
-  const int rows = p.n_tok * G;
+// A tile's K and V into a ring stage by the whole workgroup, 16 bytes a thread and row pair.
+__device__ __forceinline__ void load_tile(const TileRows& ts, uint16_t* st) {
+  const uint32_t r = threadIdx.x >> 3, c = threadIdx.x & 7;
+  const uint32_t o0 = min(r, ts.last) * ts.row + 16u * (c ^ sw(r));
+  const uint32_t o1 = min(r + 32, ts.last) * ts.row + 16u * (c ^ sw(r + 32));
+  lds_load16(ts.k + o0, st);
+  lds_load16(ts.k + o1, st + 32 * D);
+  lds_load16(ts.v + o0, st + TILE);
+  lds_load16(ts.v + o1, st + TILE + 32 * D);
+}
 
-  SeqCursor tc;
-  tc.pk = reinterpret_cast<const char*>(a.pageK + (int64_t)h * TILE);
-  tc.pv = reinterpret_cast<const char*>(a.pageV + (int64_t)h * TILE);
-  tc.fk = reinterpret_cast<const char*>(a.K + ((int64_t)p.tok0 * H + h) * D);
-  tc.fv = reinterpret_cast<const char*>(a.V + ((int64_t)p.tok0 * H + h) * D);
-  tc.page_bytes = (int64_t)H * TILE * 2;
-  tc.frame_row = 2u * (uint32_t)(H * D);
-  tc.frame_bytes = (int64_t)BK * tc.frame_row;
-  tc.entry = a.table + p.entry0;
-  tc.n_pages = p.n_pages;
-  tc.n_tiles = n_tiles;
-  tc.last_rows = p.last_rows;
-  tc.frame_rows = p.frame > 0 ? p.frame - (n_tiles - p.n_pages - 1) * BK : p.last_rows;
-  tc.r = tid >> 3;
-  tc.g0 = 16u * ((tid & 7) ^ sw(tid >> 3));
-  tc.g1 = 16u * ((tid & 7) ^ sw((tid >> 3) + 32));
-  tc.base = t0;
-  if (t0 < p.n_pages) tc.fetch_entries(t0);
-  uint16_t* const ldsw = lds + wave * 8 * D;
+// Lane l's 16 bytes at base + off go to LDS byte lds + 16 l.  (Assembly: the compiler would wait for
+// every such load in flight before each LDS read.  No register is written.  The wait states are
+// those a scalar that a vector instruction wrote needs before a load reads it.)
+__device__ __forceinline__ void lds_load16_asm(const char* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
+}
 
-  const int q0 = qt * BQ + wave * 32;  // this wave's first row of the pass
-  const bool active = q0 < rows;
-  bf16x8 qf[4];
-  {
-    const int r = min(q0 + l32, rows - 1);
-    const uint16_t* qp = a.Q + (((int64_t)p.tok0 + r / G) * H * G + h * G + r % G) * D + half * 8;
+// ---- few queries: every wave takes tiles of its own -------------------------------------------
+
+constexpr int kHalf = 32;                   // keys of a wave's stage
+constexpr int kHalfStage = 2 * kHalf * D;   // K rows then V rows: 8 KB
+constexpr int kHalfLoads = 8;               // load instructions of a stage
+static_assert(2 * 4 * kHalfStage == NSTAGE * STAGE, "four waves' two stages fill the same LDS");
+
+// Half hk (32 keys) of a tile into a wave's stage at LDS byte `st`, 8 rows an instruction.
+__device__ __forceinline__ void load_half(const TileRows& ts, int hk, uint32_t st, int lane) {
+  const uint32_t r0 = lane >> 3, c = lane & 7;
 #pragma unroll
-    for (int ds = 0; ds < 4; ++ds) qf[ds] = *reinterpret_cast<const bf16x8*>(qp + ds * 16);
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t r = 8 * i + r0;
+    const uint32_t off = min(r + kHalf * hk, ts.last) * ts.row + 16u * (c ^ sw(r));
+    lds_load16_asm(ts.k, off, st + i * 8 * D * 2);
+    lds_load16_asm(ts.v, off, st + kHalf * D * 2 + i * 8 * D * 2);
   }
+}
+
+// 32 keys for the wave's 32 queries; tile_compute's arithmetic.
+template <bool kFirst>
+__device__ __forceinline__ void half_compute(const uint16_t* stage, const bf16x8 (&qf)[4], int lane, int valid,
+                                             SoftmaxState& sm) {
+  const int l32 = lane & 31, half = lane >> 5;
+  f32x16 s = {};
+#pragma unroll
+  for (int ds = 0; ds < 4; ++ds)
+    s = mfma32(*reinterpret_cast<const bf16x8*>(&stage[swz(l32, ds * 2 + half)]), qf[ds], s);
+  if (valid < kHalf) {
+    const float fv = (float)(valid - 4 * half - 1);
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      s[r] = fmaf(__saturatef((float)(8 * (r >> 2) + (r & 3)) - fv), kNegBig, s[r]);
+  }
+  bf16x8 p[2];
+  float rsum = -0.f;
+  auto exponentials = [&]() {
+    rsum = -0.f;
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[r], kScaleLog2, -sm.m));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(s[r + 1], kScaleLog2, -sm.m));
+      rsum += e0 + e1;
+      p[r >> 3][r & 7] = (__bf16)e0;
+      p[r >> 3][(r & 7) + 1] = (__bf16)e1;
+    }
+  };
+  if (!kFirst) exponentials();
+  if (kFirst || __any(!(rsum < kOverflowGuard))) {
+    float mx = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    const float m_new = fmaxf(sm.m, half_max(mx) * kScaleLog2);
+    if (!kFirst) {
+      const float alpha = __builtin_amdgcn_exp2f(sm.m - m_new);
+      sm.l *= alpha;
+      sm.o0 *= alpha;
+      sm.o1 *= alpha;
+    }
+    sm.m = m_new;
+    exponentials();
+  }
+  sm.l += rsum;
+  // V^T through transposing reads, as in tile_compute
+  const uint16_t* vt = stage + kHalf * D;
+  const int g = lane >> 4, i16 = lane & 15, rr = i16 >> 2, jj = i16 & 3, hh = g >> 1;
+  const int col = 16 * (g & 1) + 4 * jj;
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) {
+    const int row = ks * 16 + 4 * hh + rr;
+#pragma unroll
+    for (int db = 0; db < 2; ++db) {
+      const int lcol = db * 32 + col;
+      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vt + swz(row, lcol >> 3) + (lcol & 7)));
+      const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vt + swz(row + 8, lcol >> 3) + (lcol & 7)));
+      const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      if (db == 0)
+        sm.o0 = mfma32(va, p[ks], sm.o0);
+      else
+        sm.o1 = mfma32(va, p[ks], sm.o1);
+    }
+  }
+}
+
+// ---- results ----------------------------------------------------------------------------------
+
+// A wave's 32 output rows staged in LDS as fp32, stride kRowStride (16-byte aligned; the 32 rows' pieces
+// spread over the banks).
+constexpr int kRowStride = D + 4;
+__device__ __forceinline__ void stage_rows(const SoftmaxState& sm, float* st, int lane) {
+  float* sp = st + (lane & 31) * kRowStride + 4 * (lane >> 5);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    *reinterpret_cast<float4*>(sp + 8 * j) =
+        make_float4(sm.o0[4 * j], sm.o0[4 * j + 1], sm.o0[4 * j + 2], sm.o0[4 * j + 3]);
+    *reinterpret_cast<float4*>(sp + 32 + 8 * j) =
+        make_float4(sm.o1[4 * j], sm.o1[4 * j + 1], sm.o1[4 * j + 2], sm.o1[4 * j + 3]);
+  }
+}
+
+// Eight elements d8 .. of an output row (unnormalised, row sum l, reference m): final, or into the
+// workgroup's partial slot (fp32: rounding it to bf16 would cost as much again as the output's own rounding).
+__device__ __forceinline__ void write_row(const SeqArgs& a, const SeqPass& p, int h, int r, int d8, const float (&o)[8],
+                                          float m, float l, float* slot) {
+  if (!slot) {
+    const int G = a.group, HG = a.n_heads * G, tok = r / G, head = h * G + r % G;
+    const float inv = 1.f / l;
+    const uint2 lo = to_bf16x4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    const uint2 hi = to_bf16x4(o[4] * inv, o[5] * inv, o[6] * inv, o[7] * inv);
+    *reinterpret_cast<uint4*>(a.out + (((int64_t)p.tok0 + tok) * HG + head) * D + d8) =
+        make_uint4(lo.x, lo.y, hi.x, hi.y);
+    if (d8 == 0) a.lse[(int64_t)p.tok0 * HG + (int64_t)head * p.n_tok + tok] = (m + __log2f(l)) * kLn2;
+    return;
+  }
+  const int rr = r % kSubRows;
+  float* const row = slot + rr * D + d8;
+  *reinterpret_cast<float4*>(row) = make_float4(o[0], o[1], o[2], o[3]);
+  *reinterpret_cast<float4*>(row + 4) = make_float4(o[4], o[5], o[6], o[7]);
+  if (d8 == 0) {
+    slot[kSubRows * D + rr] = m;
+    slot[kSubRows * D + kSubRows + rr] = l;
+  }
+}
+
+// A segment: tiles t0 .. t1 - 1 of one unit.
+struct Segment {
+  int h, qt, t0, t1;
+  float* slots;   // partial slots of the segment, or NULL: it is the whole unit, and final
+};
+
+__device__ __forceinline__ void load_queries(const SeqArgs& a, const SeqPass& p, int h, int q0, int lane, bf16x8 (&qf)[4]) {
+  const int G = a.group, r = min(q0 + (lane & 31), p.n_tok * G - 1);
+  const uint16_t* qp = a.Q + (((int64_t)p.tok0 + r / G) * a.n_heads * G + h * G + r % G) * D + (lane >> 5) * 8;
+#pragma unroll
+  for (int ds = 0; ds < 4; ++ds) qf[ds] = *reinterpret_cast<const bf16x8*>(qp + ds * 16);
+}
+
+// Few queries: the waves share them and take every fourth tile each, half a tile at a time through
+// two stages of their own, without barriers; the loads of the next half run under this one's work.
+__device__ __forceinline__ void narrow_segment(const SeqArgs& a, const SeqPass& p, const SeqCursor& tc, const Segment& g,
+                                               uint16_t* lds, float (*s_m)[kSubRows], float (*s_l)[kSubRows]) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
+  const int q0 = g.qt * kSubRows;
+  bf16x8 qf[4];
+  load_queries(a, p, g.h, q0, lane, qf);
   SoftmaxState sm;
   sm.m = kNegBig;
   sm.l = 0.f;
   sm.o0 = f32x16{};
   sm.o1 = f32x16{};
+  const uint32_t ring = (uint32_t)(uintptr_t)(lds_void*)(lds + wave * 2 * kHalfStage);
+  const uint16_t* const stage = lds + wave * 2 * kHalfStage;
+  const int n = g.t1 - g.t0 > wave ? (g.t1 - g.t0 - wave + 3) / 4 : 0;  // tiles of this wave
+  TileOrder order{g.t0 + wave, 4};
+  TileRows next{};
+  if (n > 0) {
+    order.fetch(tc, 0);
+    next = order.rows(tc, 0);
+  }
+  // (the queries pass through a wait here: the compiler's own for them would wait for the tiles too)
+  asm volatile("s_waitcnt vmcnt(0)" : "+v"(qf[0]), "+v"(qf[1]), "+v"(qf[2]), "+v"(qf[3])::"memory");
+  if (n > 0) {
+    load_half(next, 0, ring, lane);
+    load_half(next, 1, ring + kHalfStage * 2, lane);
+  }
+  for (int i = 0; i < n; i = uniform(i + 1)) {
+    const int valid = tc.valid(order.at(i));
+    const bool more = i + 1 < n;
+    if (more) next = order.rows(tc, i + 1);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kHalfLoads) : "memory");
+    if (i == 0)
+      half_compute<true>(stage, qf, lane, valid, sm);
+    else
+      half_compute<false>(stage, qf, lane, valid, sm);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) {
+      load_half(next, 0, ring, lane);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kHalfLoads) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    if (valid > kHalf) half_compute<false>(stage + kHalfStage, qf, lane, valid - kHalf, sm);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) load_half(next, 1, ring + kHalfStage * 2, lane);
+  }
+  // The four waves' sums meet in LDS.
+  const float l_tot = half_sum(sm.l);
+  __syncthreads();
+  float* const st = reinterpret_cast<float*>(lds);
+  stage_rows(sm, st + wave * kSubRows * kRowStride, lane);
+  if (half == 0) {
+    s_m[wave][l32] = sm.m;
+    s_l[wave][l32] = l_tot;
+  }
+  __syncthreads();
+  const int rr = tid >> 3, d8 = (tid & 7) * 8, r = q0 + rr;
+  if (r < p.n_tok * a.group) {
+    float m = s_m[0][rr];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) m = fmaxf(m, s_m[w][rr]);
+    float l = 0.f, o[8] = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = __builtin_amdgcn_exp2f(s_m[w][rr] - m);
+      l = fmaf(f, s_l[w][rr], l);
+      const float* x = st + (w * kSubRows + rr) * kRowStride + d8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = fmaf(f, x[e], o[e]);
+    }
+    write_row(a, p, g.h, r, d8, o, m, l, g.slots);
+  }
+  __syncthreads();  // (the LDS is the next segment's)
+}
 
-  // The ring of attend.hip: two tiles computed per barrier while the next two stream in.
+// The ring of attend.hip: two tiles computed per barrier while the next two stream in.
+__device__ __forceinline__ void wide_segment(const SeqArgs& a, const SeqPass& p, const SeqCursor& tc, const Segment& g,
+                                             uint16_t* lds, float (*s_m)[kSubRows], float (*s_l)[kSubRows]) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
+  const int q0 = g.qt * BQ + wave * 32, rows = p.n_tok * a.group, t0 = g.t0, t1 = g.t1;
+  bf16x8 qf[4];
+  load_queries(a, p, g.h, q0, lane, qf);
+  SoftmaxState sm;
+  sm.m = kNegBig;
+  sm.l = 0.f;
+  sm.o0 = f32x16{};
+  sm.o1 = f32x16{};
+  const bool active = q0 < rows;
+  uint16_t* const ldsw = lds + wave * 8 * D;
+  TileOrder order{t0, 1};
+  order.fetch(tc, 0);
   auto step = [&](auto phase, auto first, int t) {
     constexpr int P = decltype(phase)::value;
-    if (t + 2 < t1) tc.load(t + 2, ldsw + (P + 2) % NSTAGE * STAGE);
-    if (t + 3 < t1) tc.load(t + 3, ldsw + (P + 3) % NSTAGE * STAGE);
+    if (t + 2 < t1) load_tile(order.rows(tc, t + 2 - t0), ldsw + (P + 2) % NSTAGE * STAGE);
+    if (t + 3 < t1) load_tile(order.rows(tc, t + 3 - t0), ldsw + (P + 3) % NSTAGE * STAGE);
     if (active) {
       tile_compute<decltype(first)::value>(lds + P * STAGE, qf, lane, tc.valid(t), sm);
       if (t + 1 < t1) tile_compute<false>(lds + (P + 1) * STAGE, qf, lane, tc.valid(t + 1), sm);
@@ -137,8 +350,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
-  tc.load(t0, ldsw);
-  if (t0 + 1 < t1) tc.load(t0 + 1, ldsw + STAGE);
+  load_tile(order.rows(tc, 0), ldsw);
+  if (t0 + 1 < t1) load_tile(order.rows(tc, 1), ldsw + STAGE);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   step(StageConst<0>{}, std::true_type{}, t0);
@@ -148,119 +361,196 @@ __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
     step(StageConst<0>{}, std::false_type{}, t + 2);
   }
 
-  // Rows through LDS, as whole 128-byte rows (the ring is free: the last step ended in a barrier).
-  if (!active) return;  // uniform in the wave; no barrier follows
-  const float l_tot = half_sum(sm.l);
-  constexpr int kOutStageRow = D + 8;
-  uint16_t* const st = lds + wave * 32 * kOutStageRow;
-  {
-    const float inv = 1.f / l_tot;
-    uint16_t* sp = st + l32 * kOutStageRow + 4 * half;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      *reinterpret_cast<uint2*>(sp + 8 * j) =
-          to_bf16x4(sm.o0[4 * j] * inv, sm.o0[4 * j + 1] * inv, sm.o0[4 * j + 2] * inv, sm.o0[4 * j + 3] * inv);
-      *reinterpret_cast<uint2*>(sp + 32 + 8 * j) =
-          to_bf16x4(sm.o1[4 * j] * inv, sm.o1[4 * j + 1] * inv, sm.o1[4 * j + 2] * inv, sm.o1[4 * j + 3] * inv);
+  // Rows through LDS, so that whole rows are written (the ring is free: the last step ended in a barrier).
+  if (active) {  // uniform in the wave
+    const float l_tot = half_sum(sm.l);
+    float* const st = reinterpret_cast<float*>(lds) + wave * kSubRows * kRowStride;
+    stage_rows(sm, st, lane);
+    if (half == 0) {
+      s_m[wave][l32] = sm.m;
+      s_l[wave][l32] = l_tot;
     }
-  }
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  const int r8 = lane >> 3, c8 = (lane & 7) * 8;
-  if (p.slot0 < 0) {
-    if (half == 0 && q0 + l32 < rows) {
-      const int r = q0 + l32;
-      a.lse[(int64_t)p.tok0 * H * G + (int64_t)(h * G + r % G) * p.n_tok + r / G] = (sm.m + __log2f(l_tot)) * kLn2;
-    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    float* const slot = g.slots ? g.slots + wave * kSubFloats : nullptr;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int r = q0 + 8 * i + r8;
-      if (r < rows)
-        *reinterpret_cast<uint4*>(a.out + (((int64_t)p.tok0 + r / G) * H * G + h * G + r % G) * D + c8) =
-            *reinterpret_cast<const uint4*>(st + (8 * i + r8) * kOutStageRow + c8);
-    }
-    return;
-  }
-  const int sub = ((h * p.q_tiles + qt) * p.pieces + piece) * (BQ / kSubRows) + wave;
-  float* const ps = a.part + (int64_t)(p.slot0 + sub) * kSubFloats;
-  if (half == 0) {
-    ps[kSubRows * D / 2 + l32] = sm.m;
-    ps[kSubRows * D / 2 + kSubRows + l32] = l_tot;
-  }
-  uint16_t* const po = reinterpret_cast<uint16_t*>(ps);
+      const int rr = 8 * i + (lane >> 3), d8 = (lane & 7) * 8;
+      if (q0 + rr >= rows) continue;
+      float o[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (q0 + 8 * i + r8 < rows)
-      *reinterpret_cast<uint4*>(po + (8 * i + r8) * D + c8) =
-          *reinterpret_cast<const uint4*>(st + (8 * i + r8) * kOutStageRow + c8);
+      for (int e = 0; e < 8; ++e) o[e] = st[rr * kRowStride + d8 + e];
+      write_row(a, p, g.h, q0 + rr, d8, o, s_m[wave][rr], s_l[wave][rr], slot);
+    }
+  }
+  __syncthreads();  // (the LDS is the next segment's)
 }
 
-// Joins the pieces of 32 rows of one sequence and kv head, eight threads a row.
-__global__ __launch_bounds__(256) void seq_merge_kernel(SeqArgs a) {
-  const int H = a.n_heads, G = a.group;
-  const int ip = last_at_or_below(a.n_inner, a.n_pass, (int)blockIdx.x, [&](int i) { return a.pass[i].merge0; });
-  const SeqPass& leaf = a.pass[ip];
-  const int b = (int)blockIdx.x - leaf.merge0;
-  const int h = uniform(b % H), rb = uniform(b / H);
-  const int row = rb * kSubRows + (threadIdx.x >> 3), d8 = (threadIdx.x & 7) * 8;
-  if (row >= leaf.n_tok * G) return;
-  constexpr int kBatch = 8;  // pieces whose loads are in flight together
+__global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
+  __shared__ __attribute__((aligned(16))) uint16_t lds[NSTAGE * STAGE];
+  __shared__ float s_m[4][kSubRows], s_l[4][kSubRows];
+  // Workgroups are dealt to the XCDs in turn: consecutive chunks (query tiles of a head) share one.
+  const int per = (a.chunks + a.n_queues - 1) / a.n_queues;
+  const int c = uniform((int)blockIdx.x % a.n_queues * per + (int)blockIdx.x / a.n_queues);
+  if (c >= a.chunks) return;
+  const int begin = c * a.E, end = min(begin + a.E, a.total);
+  int ip = last_at_or_below(0, a.n_pass, begin, [&](int i) { return a.pos0[i]; });
+  for (int pos = begin; pos < end;) {  // pos: the chunk's positions from here on are still to be done
+    const SeqPass& p = a.pass[ip];
+    const int H = a.n_heads, T = seq_tiles(p), units = H * p.q_tiles;
+    Segment g;
+    int unit = 0;
+    g.t0 = T == 0 ? 0 : uniform(seq_first_tile(p, T, pos - p.pos0, &unit));
+    unit = uniform(unit);
+    if (T == 0 || unit >= units) {
+      if (++ip >= a.n_pass) break;
+      pos = max(pos, a.pos0[ip]);  // (the chunk may begin inside the last tile before it)
+      continue;
+    }
+    int end_unit = 0;
+    const int end_tile = uniform(seq_first_tile(p, T, end - p.pos0, &end_unit));
+    g.t1 = uniform(end_unit) > unit ? T : end_tile;
+    if (uniform(end_unit) < unit || g.t1 <= g.t0) break;  // the last positions belong to a tile that began before
+    // query tiles of a head are neighbours
+    g.h = uniform(unit / p.q_tiles);
+    g.qt = unit - g.h * p.q_tiles;
+    const bool shared = ip < a.n_inner || p.parent >= 0;
+    g.slots = !shared && g.t0 == 0 && g.t1 == T
+                  ? nullptr
+                  : a.part + (int64_t)seq_slot(p, shared, unit, c, uniform(seq_pos(p, unit, 0) / a.E)) * kSubFloats;
+    SeqCursor tc;
+    tc.pk = reinterpret_cast<const char*>(a.pageK + (int64_t)g.h * TILE);
+    tc.pv = reinterpret_cast<const char*>(a.pageV + (int64_t)g.h * TILE);
+    tc.fk = reinterpret_cast<const char*>(a.K + ((int64_t)p.tok0 * H + g.h) * D);
+    tc.fv = reinterpret_cast<const char*>(a.V + ((int64_t)p.tok0 * H + g.h) * D);
+    tc.page_bytes = (int64_t)H * TILE * 2;
+    tc.frame_row = 2u * (uint32_t)(H * D);
+    tc.entry = a.table + p.entry0;
+    tc.n_pages = p.n_pages;
+    tc.n_tiles = T;
+    tc.last_rows = p.last_rows;
+    tc.frame_rows = p.frame > 0 ? p.frame - (T - p.n_pages - 1) * BK : p.last_rows;
+    if (p.tile_rows == kSubRows)
+      narrow_segment(a, p, tc, g, lds, s_m, s_l);
+    else
+      wide_segment(a, p, tc, g, lds, s_m, s_l);
+    pos = g.t1 < T ? end : seq_pos(p, unit + 1, 0);
+  }
+}
+
+// Joins the segments of a sequence's rows, 16 lanes a row's 64 elements.  Where a row has many segments
+// a wave takes one row and its four groups of lanes every fourth segment each (kOne); where it has few, each
+// group takes a row of its own.
+template <bool kOne>
+__device__ __forceinline__ void merge_rows(const SeqArgs& a, const SeqPass& leaf, int ip, int h, int row) {
+  const int G = a.group, lane = threadIdx.x & 63;
+  const int grp = kOne ? lane >> 4 : 0, d4 = (lane & 15) * 4;
+  constexpr int kStep = kOne ? 4 : 1;
+  constexpr int kBatch = kOne ? 4 : 2;  // segments a lane has in flight together
+  constexpr int kLevels = 3;            // passes whose segments are taken as one list
   float mmax = kNegBig, L = 0.f;
-  float acc[8] = {};
-  for (int i = ip; i >= 0; i = a.pass[i].parent) {
-    const SeqPass& p = a.pass[i];
-    const int r = (leaf.tok0 - p.tok0) * G + row, per_tile = p.tile_rows / kSubRows;
-    const int qt = r / p.tile_rows, sub = r % p.tile_rows / kSubRows, rr = r % kSubRows;
-    const float* const first =
-        a.part + ((int64_t)p.slot0 + (int64_t)(h * p.q_tiles + qt) * p.pieces * per_tile + sub) * kSubFloats;
-    for (int j0 = 0; j0 < p.pieces; j0 += kBatch) {
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = ip; i >= 0;) {
+    // segments [count[k], count[k + 1]) of the list are level k's, `stride` slots apart; `in_slot`: the row
+    int first[kLevels], stride[kLevels], in_slot[kLevels], count[kLevels + 1];
+    count[0] = 0;
+#pragma unroll
+    for (int k = 0; k < kLevels; ++k) {
+      first[k] = stride[k] = in_slot[k] = 0;
+      count[k + 1] = count[k];
+      if (i < 0) continue;  // (uniform in the wave)
+      const SeqPass& p = a.pass[i];
+      const int T = seq_tiles(p);
+      const bool shared = i < a.n_inner || p.parent >= 0;
+      i = uniform(p.parent);
+      if (T == 0) continue;
+      const int r = (leaf.tok0 - p.tok0) * G + row;
+      const int qt = uniform(r / p.tile_rows), unit = h * p.q_tiles + qt;
+      const int c0 = uniform(seq_pos(p, unit, 0) / a.E), n = uniform(seq_pos(p, unit, T - 1) / a.E) - c0 + 1;  // its chunks
+      if (!shared && n == 1) return;  // written by the forward launch
+      stride[k] = seq_slot_step(p, shared);
+      first[k] = seq_slot(p, shared, unit, c0, c0) + r % p.tile_rows / kSubRows - count[k] * stride[k];
+      in_slot[k] = r % kSubRows;
+      count[k + 1] = count[k] + n;
+    }
+    const int n = count[kLevels];
+    for (int j0 = grp; j0 < n; j0 += kStep * kBatch) {
       float mv[kBatch], lv[kBatch];
-      uint4 v[kBatch];
+      float4 v[kBatch];
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const float* ps = first + (int64_t)min(j0 + j, p.pieces - 1) * per_tile * kSubFloats;
-        mv[j] = ps[kSubRows * D / 2 + rr];
-        lv[j] = ps[kSubRows * D / 2 + kSubRows + rr];
-        v[j] = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(ps) + rr * D + d8);
+        const int x = min(j0 + kStep * j, n - 1);
+        int slot = first[0] + x * stride[0], rr = in_slot[0];
+#pragma unroll
+        for (int k = 1; k < kLevels; ++k)
+          if (x >= count[k]) slot = first[k] + x * stride[k], rr = in_slot[k];
+        const float* ps = a.part + (int64_t)slot * kSubFloats;
+        mv[j] = ps[kSubRows * D + rr];
+        lv[j] = ps[kSubRows * D + kSubRows + rr];
+        v[j] = *reinterpret_cast<const float4*>(ps + rr * D + d4);
       }
       float m_new = mmax;
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) m_new = fmaxf(m_new, mv[j]);  // clamped copies repeat a real one
       const float scale = __builtin_amdgcn_exp2f(mmax - m_new);
       L *= scale;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] *= scale;
+      acc.x *= scale, acc.y *= scale, acc.z *= scale, acc.w *= scale;
       mmax = m_new;
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const float w = j0 + j < p.pieces ? __builtin_amdgcn_exp2f(mv[j] - mmax) * lv[j] : 0.f;
-        L += w;
-        const uint32_t wd[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          acc[2 * e] = fmaf(w, __uint_as_float(wd[e] << 16), acc[2 * e]);
-          acc[2 * e + 1] = fmaf(w, __uint_as_float(wd[e] & 0xFFFF0000u), acc[2 * e + 1]);
-        }
+        const float w = j0 + kStep * j < n ? __builtin_amdgcn_exp2f(mv[j] - mmax) : 0.f;
+        L = fmaf(w, lv[j], L);
+        acc.x = fmaf(w, v[j].x, acc.x);
+        acc.y = fmaf(w, v[j].y, acc.y);
+        acc.z = fmaf(w, v[j].z, acc.z);
+        acc.w = fmaf(w, v[j].w, acc.w);
       }
     }
   }
+  if (kOne) {
+#pragma unroll
+    for (int mask = 16; mask < 64; mask <<= 1) {
+      const float m2 = __shfl_xor(mmax, mask), m_new = fmaxf(mmax, m2);
+      const float f = __builtin_amdgcn_exp2f(mmax - m_new), f2 = __builtin_amdgcn_exp2f(m2 - m_new);
+      L = f * L + f2 * __shfl_xor(L, mask);
+      acc.x = f * acc.x + f2 * __shfl_xor(acc.x, mask);
+      acc.y = f * acc.y + f2 * __shfl_xor(acc.y, mask);
+      acc.z = f * acc.z + f2 * __shfl_xor(acc.z, mask);
+      acc.w = f * acc.w + f2 * __shfl_xor(acc.w, mask);
+      mmax = m_new;
+    }
+    if (grp != 0) return;
+  }
   const float inv = L > 0.f ? 1.f / L : 0.f;  // no key at all: zeros, and a log-sum-exp of -inf
-  const int tok = row / G, head = h * G + row % G;
-  const uint2 lo = to_bf16x4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-  const uint2 hi = to_bf16x4(acc[4] * inv, acc[5] * inv, acc[6] * inv, acc[7] * inv);
-  *reinterpret_cast<uint4*>(a.out + (((int64_t)leaf.tok0 + tok) * H * G + head) * D + d8) =
-      make_uint4(lo.x, lo.y, hi.x, hi.y);
-  if (d8 == 0)
-    a.lse[(int64_t)leaf.tok0 * H * G + (int64_t)head * leaf.n_tok + tok] =
+  const int HG = a.n_heads * G, tok = row / G, head = h * G + row % G;
+  *reinterpret_cast<uint2*>(a.out + (((int64_t)leaf.tok0 + tok) * HG + head) * D + d4) =
+      to_bf16x4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+  if (d4 == 0)
+    a.lse[(int64_t)leaf.tok0 * HG + (int64_t)head * leaf.n_tok + tok] =
         L > 0.f ? (mmax + __log2f(L)) * kLn2 : -__builtin_inff();
+}
+
+__global__ __launch_bounds__(256) void seq_merge_kernel(SeqArgs a) {
+  const int H = a.n_heads, wave = threadIdx.x >> 6;
+  const int ip = last_at_or_below(a.n_inner, a.n_pass, (int)blockIdx.x, [&](int i) { return a.merge0[i]; });
+  const SeqPass& leaf = a.pass[ip];
+  const int b = (int)blockIdx.x - a.merge0[ip];
+  const int h = uniform(b % H), row0 = uniform(b / H * leaf.merge_rows), rows = leaf.n_tok * a.group;
+  if (leaf.merge_rows == kMergeOne) {
+    if (row0 + wave < rows) merge_rows<true>(a, leaf, ip, h, uniform(row0 + wave));
+  } else {
+    const int row = row0 + (int)(threadIdx.x >> 4);  // (a block's 16 rows lie in one query tile)
+    if (row < rows) merge_rows<false>(a, leaf, ip, h, row);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_attend_seqs(const SeqArgs& a, hipStream_t s) {
-  if (a.blocks > 0) {
-    hipLaunchKernelGGL(seq_fwd_kernel, dim3((unsigned)a.blocks), dim3(kAttnThreads), 0, s, a);
+  if (a.chunks > 0) {
+    const unsigned X = (unsigned)a.n_queues, grid = ((unsigned)a.chunks + X - 1) / X * X;
+    hipLaunchKernelGGL(seq_fwd_kernel, dim3(grid), dim3(kAttnThreads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -33,7 +33,7 @@ rv_status check_current(int device, const char* what);
 
 // rv_init, and the partial slots of rv_attend_seqs.  Enough for every batch: a launch that would
 // need more takes fewer sequences.
-constexpr int64_t kSeqPartSlots = 16384;
+constexpr int64_t kSeqPartSlots = 8192;
 constexpr size_t kSeqPartFloats = (size_t)kSeqPartSlots * kSubFloats;
 rv_status setup_sequences();
 

@@ -191,23 +191,30 @@ class PageBook {
 // A pass: queries of consecutive tokens over a range of pages that all of them attend to (and,
 // for one sequence's own pass, the frame keys of its tokens).  Passes form a forest: a sequence's
 // context is its own pass (a leaf) and the passes above it.
+//
+// A unit is one query tile of one kv head of a pass; its work is the pass's key tiles, each of
+// `cost` positions, and `fixed` more before its second.  The positions of all units, one after another, are cut into chunks of E, one
+// workgroup each: a tile belongs to the chunk that its first position lies in.
 struct SeqPass {
-  int32_t block0;     // first workgroup
+  int32_t pos0;       // first position
   int32_t tok0, n_tok;
   int32_t entry0;     // table entry of the first page
   int32_t n_pages;
   int32_t last_rows;  // valid rows of the last page
   int32_t frame;      // frame keys: n_tok or 0
   int32_t parent;     // pass above, or -1
-  int32_t pieces;     // the key tiles are cut into this many pieces
   int32_t q_tiles;    // query tiles of tile_rows rows
   int32_t tile_rows;  // 128, or 32 where the pass has few queries
-  int32_t slot0;      // first partial slot (of 32 rows); -1: outputs are written directly
-  int32_t merge0;     // leaves: first workgroup of the merge launch
+  int32_t cost;       // positions of a key tile
+  int32_t fixed;      // positions of a unit's start and end
+  int32_t slot0;      // shared passes (inner ones, and leaves below one): slot of unit 0 and chunk 0
+  int32_t merge_rows; // leaves: rows a merge workgroup takes
 };
-constexpr int kMaxPasses = 72;
+constexpr int kMaxPasses = 56;
 constexpr int kSubRows = 32;  // rows of a partial slot of this launch
-constexpr int kSubFloats = kSubRows * kHeadDim / 2 + 2 * kSubRows;
+constexpr int kSubFloats = kSubRows * kHeadDim + 2 * kSubRows;  // fp32 rows, references, row sums
+constexpr int kSubsPerTile = kAttnBQ / kSubRows;
+constexpr int kMergeOne = 4, kMergeFew = 16;  // rows a merge workgroup takes: a wave one, or four
 struct SeqArgs {
   const uint16_t *Q, *K, *V;      // packed frames [tokens][Hq or H][64]; K, V NULL without frame keys
   const uint16_t *pageK, *pageV;  // [n_pages][H][64][64]
@@ -217,10 +224,35 @@ struct SeqArgs {
   float* part;
   int n_heads, group;             // kv heads, query heads to each
   int n_pass, n_inner;            // passes; the first n_inner are not leaves
-  int blocks, merge_blocks;
+  int total, E, chunks;           // positions, positions a chunk, chunks
+  int n_queues;                   // XCDs that the workgroups are dealt over
+  int merge_blocks;
+  int32_t pos0[kMaxPasses];    // the passes' first positions, again (a workgroup finds its pass by them)
+  int32_t merge0[kMaxPasses];  // leaves: first workgroup of the merge launch
   SeqPass pass[kMaxPasses];
 };
 static_assert(sizeof(SeqArgs) <= 4096, "kernel arguments");
+
+RV_HD inline int seq_tiles(const SeqPass& p) { return p.n_pages + (p.frame + kAttnBK - 1) / kAttnBK; }
+// First position of a unit's tile.
+RV_HD inline int seq_pos(const SeqPass& p, int unit, int tile) {
+  return p.pos0 + unit * (p.fixed + seq_tiles(p) * p.cost) + (tile > 0 ? p.fixed + tile * p.cost : 0);
+}
+// The first tile (returned) and unit whose position is at or after pos0 + off; the unit may be past the last.
+RV_HD inline int seq_first_tile(const SeqPass& p, int T, int off, int* unit) {
+  const int per = p.fixed + T * p.cost, u = off / per, rest = off - u * per;
+  int t = rest <= 0 ? 0 : rest <= p.fixed + p.cost ? 1 : (rest - p.fixed + p.cost - 1) / p.cost;
+  *unit = t < T ? u : u + 1;
+  return t < T ? t : 0;
+}
+// Partial slot of the segment of unit `unit` that chunk c takes, where c0 is the unit's first chunk.
+// Shared passes: a slot for each unit and chunk (their sum grows with each segment).  Other
+// units write partial results only where they are cut, and a unit of n chunks takes the n slots from
+// 2 c0 + 1 on; the next one begins in chunk c0 + n - 1 at the earliest.
+RV_HD inline int seq_slot_step(const SeqPass& p, bool shared) { return shared ? p.tile_rows / kSubRows : kSubsPerTile; }
+RV_HD inline int seq_slot(const SeqPass& p, bool shared, int unit, int c, int c0) {
+  return shared ? p.slot0 + (unit + c) * seq_slot_step(p, true) : (c0 + c + 1) * kSubsPerTile;
+}
 
 struct SeqSpan {  // one sequence of a batch, as the plan sees it
   int seq;
@@ -229,6 +261,7 @@ struct SeqSpan {  // one sequence of a batch, as the plan sees it
 
 // Plans one launch for sequences [0, n) of a batch (tokens packed in order, the first at tok0):
 // fills a's passes, returns how many of the sequences it covers (>= 1).
+// 0 if the first one alone is too large.
 int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool frame, int n_heads, int group,
               int n_cus, int64_t max_slots, SeqArgs* a);
 

@@ -436,6 +436,7 @@ rv_status rv_attend_seqs(rv_pool p, int n, const int* seqs, const int* n_tokens,
   a.part = ctx.seq_part;
   a.n_heads = p->n_heads;
   a.group = n_q_heads / p->n_heads;
+  a.n_queues = ctx.n_queues;
   int tok0 = 0;
   for (int i = 0; i < n;) {
     rv::SeqSpan span[rv::kMaxPasses];
@@ -448,6 +449,7 @@ rv_status rv_attend_seqs(rv_pool p, int n, const int* seqs, const int* n_tokens,
     if (m == 0) break;
     const int done = rv::plan_seqs(p->book, span, m, tok0, K != nullptr, p->n_heads, a.group, ctx.n_cus,
                                    (int64_t)(ctx.seq_floats / rv::kSubFloats), &a);
+    if (done == 0) return fail(RV_ERR_INVALID, "sequence %d: too many tokens over too many rows for one call", span[0].seq);
     RV_HIP(rv::launch_attend_seqs(a, (hipStream_t)stream), "attention launch");
     for (int k = 0; k < done; ++k) tok0 += span[k].n_tok;
     i = at[done - 1] + 1;

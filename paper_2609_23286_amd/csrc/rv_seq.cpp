@@ -2,6 +2,7 @@
 // frequencies, the page pool's bookkeeping and the passes of an attention over several
 // sequences.  No device calls here, so this file also builds with a host compiler alone.
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -169,6 +170,18 @@ int common_pages(const PageBook& book, int a, int b) {
   return i;
 }
 
+// Positions of a key tile and, once, of a unit: for a workgroup's 128 rows, and for 32 (where the waves
+// take tiles side by side), in about 0.35 us.  (Fixed shares of 8 to 24 and 6 to 20, tile costs of 1 to 4
+// for the narrow units and shortest chunks of 8 to 32 measured on twelve batches, from two single tokens to
+// 16 frames: these are within 4 % of the best of each but one, where narrow tiles of cost 1 and units of 20
+// are 5 % faster; without fixed shares long batches lost 10 to 40 %.)
+constexpr int kWideCost = 4, kWideFixed = 16, kNarrowCost = 2, kNarrowFixed = 12;
+constexpr int kMinChunk = 20;     // positions
+// (no chunk between a unit's first and last is without a tile of it)
+static_assert(kMinChunk >= kWideFixed + kWideCost && kMinChunk >= kNarrowFixed + kNarrowCost, "chunk length");
+constexpr int kPartialTiles = 5;  // key tiles that a unit's partial result takes as long as
+constexpr int kFewSegments = 4;   // up to which the merge takes a row in 16 lanes
+
 struct Builder {
   const PageBook& book;
   const SeqSpan* spans;
@@ -182,7 +195,7 @@ struct Builder {
   bool overflow;
 
   int64_t tiles(int64_t n_tok) const { return ceil_div64(n_tok * group, tile_rows(n_tok)); }
-  int tile_rows(int64_t) const { return kAttnBQ; }
+  int tile_rows(int64_t n_tok) const { return n_tok * group <= kSubRows ? kSubRows : kAttnBQ; }
 
   SeqPass make(int i, int j, int p0, int p1, int parent) const {
     SeqPass p{};
@@ -216,8 +229,11 @@ struct Builder {
     for (int k = i + 1; k + 1 < j; ++k) shared = std::min(shared, common[k]);
     int64_t apart = 0;
     for (int k = i; k < j; ++k) apart += tiles(spans[k].n_tok);
-    const int64_t saved = (apart - tiles(tok[j] - tok[i])) * (shared - p0);
-    if (saved > 0) {
+    const int64_t joint = tiles(tok[j] - tok[i]);
+    // Worth a pass if it saves more tiles than the partial results cost that every unit then writes
+    // and the merge reads.
+    const int64_t saved = (apart - joint) * (shared - p0);
+    if (saved > kPartialTiles * (apart + joint)) {
       if (n_leaf + n_inner >= kMaxPasses) {
         overflow = true;
         return;
@@ -259,36 +275,47 @@ int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool 
     a->n_inner = b.n_inner;
     a->n_pass = b.n_inner + b.n_leaf;
     std::copy(b.leaf, b.leaf + b.n_leaf, a->pass + b.n_inner);
-    int64_t work = 0;
-    auto key_tiles = [](const SeqPass& p) { return p.n_pages + (int)ceil_div64(p.frame, kPageRows); };
-    for (int i = 0; i < a->n_pass; ++i) work += (int64_t)a->pass[i].q_tiles * key_tiles(a->pass[i]) * n_heads;
-    // Pieces of about the same length, so many that the device's workgroup slots are filled.
-    constexpr int kMinTiles = 4;
-    int64_t e = std::max<int64_t>(kMinTiles, ceil_div64(work, (int64_t)kAttnWgPerCu * n_cus));
-    int64_t slots = 0;
-    for (;; e *= 2) {
-      int64_t blocks = 0, merge = 0;
-      slots = 0;
-      int most = 0;
-      for (int i = 0; i < a->n_pass; ++i) {
-        SeqPass& p = a->pass[i];
-        const bool is_leaf = i >= a->n_inner;
-        p.pieces = (int)std::max<int64_t>(1, ceil_div64(key_tiles(p), e));
-        const bool direct = is_leaf && p.parent < 0 && p.pieces == 1 && key_tiles(p) > 0;
-        if (key_tiles(p) == 0) p.pieces = 0;
-        most = std::max(most, p.pieces);
-        p.block0 = (int)blocks;
-        blocks += (int64_t)p.pieces * p.q_tiles * n_heads;
-        p.slot0 = direct ? -1 : (int)slots;
-        if (!direct) slots += (int64_t)p.pieces * p.q_tiles * n_heads * (p.tile_rows / kSubRows);
-        p.merge0 = (int)merge;
-        if (is_leaf && !direct) merge += ceil_div64((int64_t)p.n_tok * group, kSubRows) * n_heads;
-      }
-      a->blocks = (int)blocks;
-      a->merge_blocks = (int)merge;
-      if (slots <= max_slots || most <= 1) break;
+    int64_t pos = 0;
+    bool fits = true;
+    for (int i = 0; i < a->n_pass; ++i) {
+      SeqPass& p = a->pass[i];
+      const bool narrow = p.tile_rows == kSubRows;
+      p.cost = narrow ? kNarrowCost : kWideCost;
+      p.fixed = seq_tiles(p) == 0 ? 0 : narrow ? kNarrowFixed : kWideFixed;
+      a->pos0[i] = p.pos0 = (int)std::min<int64_t>(pos, INT32_MAX);
+      pos += (int64_t)p.q_tiles * n_heads * (p.fixed + (int64_t)seq_tiles(p) * p.cost);
     }
-    if (slots <= max_slots || n == 1) return n;
+    if (pos > INT32_MAX / 2) {
+      if (n == 1) return 0;
+      continue;
+    }
+    // Chunks of equal length, one for each of the device's workgroup slots, but no shorter than
+    // kMinChunk.
+    a->total = (int)pos;
+    a->E = (int)std::max<int64_t>(kMinChunk, ceil_div64(pos, (int64_t)kAttnWgPerCu * n_cus));
+    a->chunks = (int)ceil_div64(pos, a->E);
+    int64_t slots = (2 * (int64_t)a->chunks + 1) * kSubsPerTile, merge = 0;
+    for (int i = 0; i < a->n_pass; ++i) {
+      SeqPass& p = a->pass[i];
+      const int units = p.q_tiles * n_heads, T = seq_tiles(p);
+      const bool leaf = i >= a->n_inner, shared = !leaf || p.parent >= 0;
+      if (shared && T > 0) {
+        const int first = p.pos0 / a->E, last = seq_pos(p, units - 1, T - 1) / a->E;
+        p.slot0 = (int)(slots - (int64_t)first * (p.tile_rows / kSubRows));
+        slots += (int64_t)(units + last - first) * (p.tile_rows / kSubRows);
+        fits = fits && slots <= max_slots;
+      }
+      a->merge0[i] = (int)merge;
+      if (!leaf) continue;
+      // merged: sums in parts, or none at all
+      int most = T == 0 ? 2 : 1;
+      for (int u = 0; u < units && T > 0; ++u)
+        most = std::max(most, seq_pos(p, u, T - 1) / a->E - seq_pos(p, u, 0) / a->E + 1);
+      p.merge_rows = shared || most > kFewSegments ? kMergeOne : kMergeFew;
+      if (shared || most > 1) merge += ceil_div64((int64_t)p.n_tok * group, p.merge_rows) * n_heads;
+    }
+    a->merge_blocks = (int)merge;
+    if (n == 1 || (fits && slots <= max_slots)) return n;
   }
 }
 

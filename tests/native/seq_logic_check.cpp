@@ -145,36 +145,87 @@ struct World {
     std::vector<rv::SeqSpan> span;
     for (int s : all) span.push_back({s, uniform(0, 3) ? uniform(1, 4) : uniform(1, 700)});
     int tok0 = uniform(0, 50);
-    const int64_t max_slots = uniform(0, 3) ? 16384 : 64;
+    const int64_t max_slots = uniform(0, 3) ? 8192 : 300;
     for (size_t i = 0; i < span.size();) {
       rv::SeqArgs a{};
       const int done = rv::plan_seqs(book, &span[i], (int)(span.size() - i), tok0, frame, n_heads, group,
                                      uniform(1, 300), max_slots, &a);
       CHECK(done >= 1 && done <= (int)(span.size() - i), "sequences covered");
       CHECK(a.n_pass <= rv::kMaxPasses && a.n_pass - a.n_inner == done, "passes");
-      std::vector<char> used(max_slots, 0);
-      int block = 0, merge = 0;
-      for (int k = 0; k < a.n_pass; ++k) {
-        const rv::SeqPass& p = a.pass[k];
-        const int tiles = p.n_pages + (p.frame + 63) / 64;
-        CHECK(p.block0 == block, "first workgroup");
-        CHECK((int64_t)p.q_tiles * p.tile_rows >= (int64_t)p.n_tok * group, "query tiles");
-        CHECK(p.pieces <= tiles && (p.pieces > 0) == (tiles > 0), "pieces");
-        CHECK(p.parent < a.n_inner && (k < a.n_inner ? p.parent < k : true), "parent");
-        block += p.pieces * p.q_tiles * n_heads;
-        if (p.slot0 >= 0) {
-          const int64_t n = (int64_t)p.pieces * p.q_tiles * n_heads * (p.tile_rows / rv::kSubRows);
-          CHECK(p.slot0 + n <= max_slots, "slots past the end");
-          for (int64_t s = p.slot0; s < p.slot0 + n && s < max_slots; ++s) CHECK(!used[s]++, "slot used twice");
-        } else {
-          CHECK(k >= a.n_inner && p.parent < 0 && p.pieces == 1, "a direct pass");
-        }
-        if (k >= a.n_inner) {
-          CHECK(p.merge0 == merge, "first merge workgroup");
-          if (p.slot0 >= 0) merge += (p.n_tok * group + rv::kSubRows - 1) / rv::kSubRows * n_heads;
+      CHECK(a.E > 0 && (int64_t)a.chunks * a.E >= a.total && (int64_t)(a.chunks - 1) * a.E < a.total, "chunks");
+      // the segments, as the kernel walks them
+      std::set<std::vector<int>> tiles_done;
+      std::map<int, std::vector<int>> slot_of;       // sub-slot -> pass, unit
+      std::map<std::vector<int>, int> segments;      // pass, unit, chunk -> slot, or -1: final
+      auto last_below = [&](int x) {
+        int i = -1;
+        while (i + 1 < a.n_pass && a.pass[i + 1].pos0 <= x) ++i;
+        return i;
+      };
+      for (int c = 0; c < a.chunks; ++c) {
+        const int begin = c * a.E, end = std::min(begin + a.E, a.total);
+        int ip = last_below(begin);
+        for (int pos = begin; pos < end;) {
+          const rv::SeqPass& p = a.pass[ip];
+          const int T = rv::seq_tiles(p), units = n_heads * p.q_tiles;
+          int unit = 0, end_unit = 0;
+          const int t0 = T == 0 ? 0 : rv::seq_first_tile(p, T, pos - p.pos0, &unit);
+          if (T == 0 || unit >= units) {
+            if (++ip >= a.n_pass) break;
+            pos = std::max(pos, a.pass[ip].pos0);
+            continue;
+          }
+          const int end_tile = rv::seq_first_tile(p, T, end - p.pos0, &end_unit);
+          const int t1 = end_unit > unit ? T : end_tile;
+          if (end_unit < unit || t1 <= t0) break;
+          const bool shared = ip < a.n_inner || p.parent >= 0;
+          CHECK(t0 >= 0 && t0 < t1 && unit >= 0 && unit < units, "a segment outside its unit");
+          for (int t = t0; t < t1; ++t) {
+            CHECK(tiles_done.insert({ip, unit, t}).second, "a tile taken twice");
+            CHECK(rv::seq_pos(p, unit, t) / a.E == c, "a tile of another chunk");
+          }
+          int slot = -1;
+          if (shared || t0 > 0 || t1 < T) {
+            slot = rv::seq_slot(p, shared, unit, c, rv::seq_pos(p, unit, 0) / a.E);
+            for (int q = slot; q < slot + p.tile_rows / rv::kSubRows; ++q) {
+              CHECK(q >= 0 && (q < max_slots || done == 1), "slot %d", q);
+              CHECK(slot_of.emplace(q, std::vector<int>{ip, unit, c}).second, "slot %d used twice", q);
+            }
+          }
+          segments[{ip, unit, c}] = slot;
+          pos = t1 < T ? end : rv::seq_pos(p, unit + 1, 0);
         }
       }
-      CHECK(block == a.blocks && merge == a.merge_blocks, "workgroups");
+      int merge = 0, pos = 0;
+      for (int k = 0; k < a.n_pass; ++k) {
+        const rv::SeqPass& p = a.pass[k];
+        const int T = rv::seq_tiles(p), units = n_heads * p.q_tiles;
+        CHECK(p.pos0 == pos && a.pos0[k] == pos && p.cost > 0, "first position");
+        pos += units * (p.fixed + T * p.cost);
+        CHECK((int64_t)p.q_tiles * p.tile_rows >= (int64_t)p.n_tok * group, "query tiles");
+        CHECK(p.parent < a.n_inner && (k < a.n_inner ? p.parent < k : true), "parent");
+        bool parts = T == 0;
+        for (int u = 0; u < units; ++u) {
+          for (int t = 0; t < T; ++t) CHECK(tiles_done.count({k, u, t}), "a tile left out");
+          if (T == 0) continue;
+          // as the merge finds them
+          const bool shared = k < a.n_inner || p.parent >= 0;
+          const int c0 = rv::seq_pos(p, u, 0) / a.E, n = rv::seq_pos(p, u, T - 1) / a.E - c0 + 1;
+          parts = parts || shared || n > 1;
+          for (int c = c0; c < c0 + n; ++c) {
+            CHECK(segments.count({k, u, c}), "a segment left out");
+            const int want = !shared && n == 1 ? -1 : rv::seq_slot(p, shared, u, c0, c0) + (c - c0) * rv::seq_slot_step(p, shared);
+            CHECK((segments[{k, u, c}]) == want, "the merge reads another slot");
+          }
+        }
+        if (k >= a.n_inner) {
+          CHECK(a.merge0[k] == merge, "first merge workgroup");
+          if (parts) merge += (p.n_tok * group + p.merge_rows - 1) / p.merge_rows * n_heads;
+          // (16 rows of a merge workgroup are in one query tile)
+          CHECK(p.merge_rows == rv::kMergeOne || (p.merge_rows == rv::kMergeFew && p.parent < 0), "merge rows");
+        }
+      }
+      CHECK(pos == a.total && merge == a.merge_blocks, "workgroups");
       for (int k = 0; k < done; ++k) {  // the pages from the leaf up are the sequence's, in order
         const rv::SeqSpan& s = span[i + k];
         const rv::SeqPass& leaf = a.pass[a.n_inner + k];
