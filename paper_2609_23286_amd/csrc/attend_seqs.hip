@@ -119,59 +119,75 @@ static_assert(2 * 4 * kHalfStage == NSTAGE * STAGE, "four waves' two stages fill
 // Half hk (32 keys) of a tile into a wave's stage at LDS byte `st`, 8 rows an instruction.
 __device__ __forceinline__ void load_half(const TileRows& ts, int hk, uint32_t st, int lane) {
   const uint32_t r0 = lane >> 3, c = lane & 7;
+  if (ts.last == BK - 1) {  // uniform: two thread offsets (the swizzle alternates) beside scalar bases
+    const uint32_t o = r0 * ts.row, o0 = o + 16u * (c ^ sw(r0)), o1 = o + 16u * (c ^ sw(r0 + 8));
+    const int64_t at = (int64_t)(kHalf * hk) * ts.row, step = 8 * (int64_t)ts.row;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t r = 8 * i + r0;
-    const uint32_t off = min(r + kHalf * hk, ts.last) * ts.row + 16u * (c ^ sw(r));
-    lds_load16_asm(ts.k, off, st + i * 8 * D * 2);
-    lds_load16_asm(ts.v, off, st + kHalf * D * 2 + i * 8 * D * 2);
+    for (int i = 0; i < 4; ++i) {
+      lds_load16_asm(ts.k + at + i * step, i & 1 ? o1 : o0, st + i * 8 * D * 2);
+      lds_load16_asm(ts.v + at + i * step, i & 1 ? o1 : o0, st + kHalf * D * 2 + i * 8 * D * 2);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t r = 8 * i + r0;
+      const uint32_t off = min(r + kHalf * hk, ts.last) * ts.row + 16u * (c ^ sw(r));
+      lds_load16_asm(ts.k, off, st + i * 8 * D * 2);
+      lds_load16_asm(ts.v, off, st + kHalf * D * 2 + i * 8 * D * 2);
+    }
   }
 }
 
-// 32 keys for the wave's 32 queries; tile_compute's arithmetic.
-template <bool kFirst>
-__device__ __forceinline__ void half_compute(const uint16_t* stage, const bf16x8 (&qf)[4], int lane, int valid,
-                                             SoftmaxState& sm) {
+// 32 keys for the wave's NQ blocks of 32 queries; tile_compute's arithmetic.  Each fragment read from LDS
+// serves all blocks.  (Before the first keys the reference is kNegBig: every p is then infinite and
+// the exact path sets it.)
+template <int NQ>
+__device__ __forceinline__ void half_compute(const uint16_t* stage, const bf16x8 (&qf)[NQ][4], int lane, int valid,
+                                             SoftmaxState (&sm)[NQ]) {
   const int l32 = lane & 31, half = lane >> 5;
-  f32x16 s = {};
+  bf16x8 kf[4];
 #pragma unroll
-  for (int ds = 0; ds < 4; ++ds)
-    s = mfma32(*reinterpret_cast<const bf16x8*>(&stage[swz(l32, ds * 2 + half)]), qf[ds], s);
-  if (valid < kHalf) {
-    const float fv = (float)(valid - 4 * half - 1);
+  for (int ds = 0; ds < 4; ++ds) kf[ds] = *reinterpret_cast<const bf16x8*>(&stage[swz(l32, ds * 2 + half)]);
+  bf16x8 p[NQ][2];
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      s[r] = fmaf(__saturatef((float)(8 * (r >> 2) + (r & 3)) - fv), kNegBig, s[r]);
-  }
-  bf16x8 p[2];
-  float rsum = -0.f;
-  auto exponentials = [&]() {
-    rsum = -0.f;
+  for (int b = 0; b < NQ; ++b) {
+    f32x16 s = {};
 #pragma unroll
-    for (int r = 0; r < 16; r += 2) {
-      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[r], kScaleLog2, -sm.m));
-      const float e1 = __builtin_amdgcn_exp2f(fmaf(s[r + 1], kScaleLog2, -sm.m));
-      rsum += e0 + e1;
-      p[r >> 3][r & 7] = (__bf16)e0;
-      p[r >> 3][(r & 7) + 1] = (__bf16)e1;
+    for (int ds = 0; ds < 4; ++ds) s = mfma32(kf[ds], qf[b][ds], s);
+    if (valid < kHalf) {
+      const float fv = (float)(valid - 4 * half - 1);
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        s[r] = fmaf(__saturatef((float)(8 * (r >> 2) + (r & 3)) - fv), kNegBig, s[r]);
     }
-  };
-  if (!kFirst) exponentials();
-  if (kFirst || __any(!(rsum < kOverflowGuard))) {
-    float mx = s[0];
+    float rsum;
+    auto exponentials = [&]() {
+      rsum = -0.f;
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-    const float m_new = fmaxf(sm.m, half_max(mx) * kScaleLog2);
-    if (!kFirst) {
-      const float alpha = __builtin_amdgcn_exp2f(sm.m - m_new);
-      sm.l *= alpha;
-      sm.o0 *= alpha;
-      sm.o1 *= alpha;
-    }
-    sm.m = m_new;
+      for (int r = 0; r < 16; r += 2) {
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[r], kScaleLog2, -sm[b].m));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[r + 1], kScaleLog2, -sm[b].m));
+        rsum += e0 + e1;
+        p[b][r >> 3][r & 7] = (__bf16)e0;
+        p[b][r >> 3][(r & 7) + 1] = (__bf16)e1;
+      }
+    };
     exponentials();
+    if (__any(!(rsum < kOverflowGuard))) {
+      float mx = s[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+      const float m_new = fmaxf(sm[b].m, half_max(mx) * kScaleLog2);
+      const float alpha = __builtin_amdgcn_exp2f(sm[b].m - m_new);
+      sm[b].l *= alpha;
+      sm[b].o0 *= alpha;
+      sm[b].o1 *= alpha;
+      sm[b].m = m_new;
+      exponentials();
+    }
+    sm[b].l += rsum;
+    if (NQ > 1) __builtin_amdgcn_sched_barrier(0);  // (one block's scores at a time: registers)
   }
-  sm.l += rsum;
   // V^T through transposing reads, as in tile_compute
   const uint16_t* vt = stage + kHalf * D;
   const int g = lane >> 4, i16 = lane & 15, rr = i16 >> 2, jj = i16 & 3, hh = g >> 1;
@@ -185,10 +201,13 @@ __device__ __forceinline__ void half_compute(const uint16_t* stage, const bf16x8
       const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vt + swz(row, lcol >> 3) + (lcol & 7)));
       const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vt + swz(row + 8, lcol >> 3) + (lcol & 7)));
       const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-      if (db == 0)
-        sm.o0 = mfma32(va, p[ks], sm.o0);
-      else
-        sm.o1 = mfma32(va, p[ks], sm.o1);
+#pragma unroll
+      for (int b = 0; b < NQ; ++b) {
+        if (db == 0)
+          sm[b].o0 = mfma32(va, p[b][ks], sm[b].o0);
+        else
+          sm[b].o1 = mfma32(va, p[b][ks], sm[b].o1);
+      }
     }
   }
 }
@@ -248,17 +267,21 @@ __device__ __forceinline__ void load_queries(const SeqArgs& a, const SeqPass& p,
 
 // Few queries: the waves share them and take every fourth tile each, half a tile at a time through
 // two stages of their own, without barriers; the loads of the next half run under this one's work.
+template <int NQ>
 __device__ __forceinline__ void narrow_segment(const SeqArgs& a, const SeqPass& p, const SeqCursor& tc, const Segment& g,
                                                uint16_t* lds, float (*s_m)[kSubRows], float (*s_l)[kSubRows]) {
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
-  const int q0 = g.qt * kSubRows;
-  bf16x8 qf[4];
-  load_queries(a, p, g.h, q0, lane, qf);
-  SoftmaxState sm;
-  sm.m = kNegBig;
-  sm.l = 0.f;
-  sm.o0 = f32x16{};
-  sm.o1 = f32x16{};
+  const int q0 = g.qt * NQ * kSubRows;
+  bf16x8 qf[NQ][4];
+  SoftmaxState sm[NQ];
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+    load_queries(a, p, g.h, q0 + b * kSubRows, lane, qf[b]);
+    sm[b].m = kNegBig;
+    sm[b].l = 0.f;
+    sm[b].o0 = f32x16{};
+    sm[b].o1 = f32x16{};
+  }
   const uint32_t ring = (uint32_t)(uintptr_t)(lds_void*)(lds + wave * 2 * kHalfStage);
   const uint16_t* const stage = lds + wave * 2 * kHalfStage;
   const int n = g.t1 - g.t0 > wave ? (g.t1 - g.t0 - wave + 3) / 4 : 0;  // tiles of this wave
@@ -269,7 +292,9 @@ __device__ __forceinline__ void narrow_segment(const SeqArgs& a, const SeqPass& 
     next = order.rows(tc, 0);
   }
   // (the queries pass through a wait here: the compiler's own for them would wait for the tiles too)
-  asm volatile("s_waitcnt vmcnt(0)" : "+v"(qf[0]), "+v"(qf[1]), "+v"(qf[2]), "+v"(qf[3])::"memory");
+#pragma unroll
+  for (int b = 0; b < NQ; ++b)
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(qf[b][0]), "+v"(qf[b][1]), "+v"(qf[b][2]), "+v"(qf[b][3])::"memory");
   if (n > 0) {
     load_half(next, 0, ring, lane);
     load_half(next, 1, ring + kHalfStage * 2, lane);
@@ -279,10 +304,7 @@ __device__ __forceinline__ void narrow_segment(const SeqArgs& a, const SeqPass& 
     const bool more = i + 1 < n;
     if (more) next = order.rows(tc, i + 1);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kHalfLoads) : "memory");
-    if (i == 0)
-      half_compute<true>(stage, qf, lane, valid, sm);
-    else
-      half_compute<false>(stage, qf, lane, valid, sm);
+    half_compute<NQ>(stage, qf, lane, valid, sm);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) {
       load_half(next, 0, ring, lane);
@@ -290,35 +312,38 @@ __device__ __forceinline__ void narrow_segment(const SeqArgs& a, const SeqPass& 
     } else {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
-    if (valid > kHalf) half_compute<false>(stage + kHalfStage, qf, lane, valid - kHalf, sm);
+    if (valid > kHalf) half_compute<NQ>(stage + kHalfStage, qf, lane, valid - kHalf, sm);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) load_half(next, 1, ring + kHalfStage * 2, lane);
   }
-  // The four waves' sums meet in LDS.
-  const float l_tot = half_sum(sm.l);
-  __syncthreads();
+  // The four waves' sums meet in LDS, a block of queries at a time.
   float* const st = reinterpret_cast<float*>(lds);
-  stage_rows(sm, st + wave * kSubRows * kRowStride, lane);
-  if (half == 0) {
-    s_m[wave][l32] = sm.m;
-    s_l[wave][l32] = l_tot;
-  }
-  __syncthreads();
-  const int rr = tid >> 3, d8 = (tid & 7) * 8, r = q0 + rr;
-  if (r < p.n_tok * a.group) {
-    float m = s_m[0][rr];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) m = fmaxf(m, s_m[w][rr]);
-    float l = 0.f, o[8] = {};
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = __builtin_amdgcn_exp2f(s_m[w][rr] - m);
-      l = fmaf(f, s_l[w][rr], l);
-      const float* x = st + (w * kSubRows + rr) * kRowStride + d8;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = fmaf(f, x[e], o[e]);
+  for (int b = 0; b < NQ; ++b) {
+    const float l_tot = half_sum(sm[b].l);
+    __syncthreads();
+    stage_rows(sm[b], st + wave * kSubRows * kRowStride, lane);
+    if (half == 0) {
+      s_m[wave][l32] = sm[b].m;
+      s_l[wave][l32] = l_tot;
     }
-    write_row(a, p, g.h, r, d8, o, m, l, g.slots);
+    __syncthreads();
+    const int rr = tid >> 3, d8 = (tid & 7) * 8, r = q0 + b * kSubRows + rr;
+    if (r < p.n_tok * a.group) {
+      float m = s_m[0][rr];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) m = fmaxf(m, s_m[w][rr]);
+      float l = 0.f, o[8] = {};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(s_m[w][rr] - m);
+        l = fmaf(f, s_l[w][rr], l);
+        const float* x = st + (w * kSubRows + rr) * kRowStride + d8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = fmaf(f, x[e], o[e]);
+      }
+      write_row(a, p, g.h, r, d8, o, m, l, g.slots ? g.slots + b * kSubFloats : nullptr);
+    }
   }
   __syncthreads();  // (the LDS is the next segment's)
 }
@@ -390,10 +415,8 @@ __device__ __forceinline__ void wide_segment(const SeqArgs& a, const SeqPass& p,
 __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
   __shared__ __attribute__((aligned(16))) uint16_t lds[NSTAGE * STAGE];
   __shared__ float s_m[4][kSubRows], s_l[4][kSubRows];
-  // Workgroups are dealt to the XCDs in turn: consecutive chunks (query tiles of a head) share one.
-  const int per = (a.chunks + a.n_queues - 1) / a.n_queues;
-  const int c = uniform((int)blockIdx.x % a.n_queues * per + (int)blockIdx.x / a.n_queues);
-  if (c >= a.chunks) return;
+  const int c = uniform(seq_chunk_of(a, (int)blockIdx.x));
+  if (c < 0) return;
   const int begin = c * a.E, end = min(begin + a.E, a.total);
   int ip = last_at_or_below(0, a.n_pass, begin, [&](int i) { return a.pos0[i]; });
   for (int pos = begin; pos < end;) {  // pos: the chunk's positions from here on are still to be done
@@ -432,7 +455,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
     tc.last_rows = p.last_rows;
     tc.frame_rows = p.frame > 0 ? p.frame - (T - p.n_pages - 1) * BK : p.last_rows;
     if (p.tile_rows == kSubRows)
-      narrow_segment(a, p, tc, g, lds, s_m, s_l);
+      narrow_segment<1>(a, p, tc, g, lds, s_m, s_l);
     else
       wide_segment(a, p, tc, g, lds, s_m, s_l);
     pos = g.t1 < T ? end : seq_pos(p, unit + 1, 0);
@@ -549,8 +572,7 @@ __global__ __launch_bounds__(256) void seq_merge_kernel(SeqArgs a) {
 
 hipError_t launch_attend_seqs(const SeqArgs& a, hipStream_t s) {
   if (a.chunks > 0) {
-    const unsigned X = (unsigned)a.n_queues, grid = ((unsigned)a.chunks + X - 1) / X * X;
-    hipLaunchKernelGGL(seq_fwd_kernel, dim3(grid), dim3(kAttnThreads), 0, s, a);
+    hipLaunchKernelGGL(seq_fwd_kernel, dim3((unsigned)seq_grid(a)), dim3(kAttnThreads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -40,14 +40,16 @@ __global__ __launch_bounds__(64) void table_kernel(TableArgs a) {
 __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a) {
   const AppendSeq& s = a.seq[my_seq(a.seq, a.n_seqs)];
   const int H = a.n_heads, block = (int)blockIdx.x - s.block0;
-  if (block == 0 && threadIdx.x < 2 && (s.fresh >> threadIdx.x & 1)) a.table[s.entry0 + threadIdx.x] = s.page[threadIdx.x];
+  if (block == 0)
+    for (int i = s.write0 + threadIdx.x; i < s.write0 + s.writes; i += NT)
+      a.table[s.entry0 + i] = i == 0 ? s.page[0] : s.page[1] + i - 1;
   const int64_t r = (int64_t)block * kRowsPerBlock + (threadIdx.x >> 3);
   const int e = 8 * (threadIdx.x & 7);
   const int skip = s.cow >= 0 ? 0 : s.offset;  // rows of the first page that stay
   const int64_t rows = (int64_t)(s.offset + s.n - skip) * H;
   if (r >= rows) return;
   const int i = skip + (int)(r / H), h = (int)(r % H), p = i / kPageRows;
-  const int page = p < 2 ? s.page[p] : a.table[s.entry0 + p];
+  const int page = p == 0 ? s.page[0] : p == 1 || s.in_a_row ? s.page[1] + p - 1 : a.table[s.entry0 + p];
   const int64_t to = page_at(page, H, h, i % kPageRows) + e;
   uint4 k, v;
   if (i < s.offset) {
@@ -86,10 +88,13 @@ __global__ __launch_bounds__(NT) void gather_kernel(GatherArgs a) {
 // The kept rows of a sequence to its new pages.
 __global__ __launch_bounds__(NT) void compact_kernel(CompactArgs a) {
   const CompactSeq& s = a.seq[my_seq(a.seq, a.n_seqs)];
-  const int H = a.n_heads;
-  const int64_t r = (int64_t)((int)blockIdx.x - s.block0) * kRowsPerBlock + (threadIdx.x >> 3);
+  const int H = a.n_heads, block = (int)blockIdx.x - s.block0;
+  const int64_t r = (int64_t)block * kRowsPerBlock + (threadIdx.x >> 3);
   const int e = 8 * (threadIdx.x & 7);
-  const int per_head = s.offset + s.n;
+  const int per_head = s.offset + s.n, leading = s.base / kPageRows;
+  if (block == 0 && s.page0 >= 0)
+    for (int i = (int)threadIdx.x - leading; i < (per_head + kPageRows - 1) / kPageRows; i += NT)
+      a.table[s.new0 + i] = i < 0 ? a.table[s.old0 + leading + i] : s.page0 + i;
   if (r >= (int64_t)per_head * H) return;
   const int h = (int)(r / per_head), i = (int)(r - (int64_t)h * per_head);
   int row = s.base + i;
@@ -103,7 +108,8 @@ __global__ __launch_bounds__(NT) void compact_kernel(CompactArgs a) {
     k = *reinterpret_cast<const uint4*>(a.K + from);
     v = *reinterpret_cast<const uint4*>(a.V + from);
   }
-  const int64_t to = page_at(a.table[s.new0 + i / kPageRows], H, h, i % kPageRows) + e;
+  const int page = s.page0 >= 0 ? s.page0 + i / kPageRows : a.table[s.new0 + i / kPageRows];
+  const int64_t to = page_at(page, H, h, i % kPageRows) + e;
   *reinterpret_cast<uint4*>(a.K + to) = k;
   *reinterpret_cast<uint4*>(a.V + to) = v;
 }

@@ -19,7 +19,7 @@ constexpr int kMaxGridBlocks = 1 << 23;
 
 constexpr int kMaxFreqs = kHeadDim / 2;
 constexpr int kPrepThreads = 256;
-constexpr int kPrepMaxTokens = 8;  // tokens a wave takes at a time
+constexpr int kPrepMaxTokens = 16;  // tokens a wave takes at a time
 
 // Source and gradient rows are [n_tokens] rows of `stride` elements, head h at column 64 h.
 struct PrepArgs {
@@ -65,13 +65,14 @@ struct TableArgs {
 };
 
 // Rows written to sequences: sequence i's rows start at `start`, `n` of them from row src_row of
-// the packed frame.  The first two pages they touch are given here (and entered into the table
-// where new); later ones were entered by an earlier launch.
+// the packed frame.  The page that holds row `start` and the one after it are given here; the pages after
+// that follow the second in number (their entries are written here), or were entered by an earlier launch.
 struct AppendSeq {
   int32_t block0;     // its first workgroup
   int32_t entry0;     // table entry of the page that holds row `start`
   int32_t page[2];
-  int32_t fresh;      // bit i: page[i] is new, its entry is written here
+  int32_t write0, writes;  // entries written here: those of pages write0 .. write0 + writes - 1 of the ones touched
+  int32_t in_a_row;   // the pages after the second are given by its number
   int32_t cow;        // page whose rows before `start` are copied to page[0], or -1
   int32_t offset;     // start % 64
   int32_t n;
@@ -116,12 +117,14 @@ struct CompactSeq {
   int32_t offset;
   int32_t n;           // kept rows after `offset`
   int32_t lo, hi;      // rows that `keep` may name: [lo, hi)
+  int32_t page0;       // new pages are page0, page0 + 1, ..., and the new table row is written here (the
+                       //   `base` / 64 entries before them copied); -1: an earlier launch wrote it
   int64_t keep0;       // sum of H n over earlier sequences
 };
 constexpr int kMaxCompact = 64;
 struct CompactArgs {
   uint16_t *K, *V;
-  const int32_t* table;
+  int32_t* table;
   const int32_t* keep;
   int n_heads, n_seqs, blocks;
   CompactSeq seq[kMaxCompact];
@@ -151,6 +154,7 @@ class PageBook {
   int32_t entry0(int s) const { return (2 * s + side_[s]) * width_; }
   int32_t page(int s, int i) const { return table_[entry0(s) + i]; }
   const int32_t* list(int s) const { return table_ + entry0(s); }
+  bool in_a_row(int s, int from) const;  // pages from index `from` on are consecutive numbers
   int users(int page) const { return refs_[page]; }
   // True once for every sequence of a batch: begin_batch() first.
   void begin_batch() { ++batch_; }
@@ -225,6 +229,7 @@ struct SeqArgs {
   int n_heads, group;             // kv heads, query heads to each
   int n_pass, n_inner;            // passes; the first n_inner are not leaves
   int total, E, chunks;           // positions, positions a chunk, chunks
+  int inner_chunks;               // chunks that begin in an inner pass
   int n_queues;                   // XCDs that the workgroups are dealt over
   int merge_blocks;
   int32_t pos0[kMaxPasses];    // the passes' first positions, again (a workgroup finds its pass by them)
@@ -245,6 +250,26 @@ RV_HD inline int seq_first_tile(const SeqPass& p, int T, int off, int* unit) {
   *unit = t < T ? u : u + 1;
   return t < T ? t : 0;
 }
+// The chunk of a workgroup, or -1.  Workgroups are dealt to the XCDs in turn; consecutive chunks (query
+// tiles of a head) go to one XCD, and each XCD gets its share of the inner passes' chunks, which are
+// bound by arithmetic, and of the leaves', which are bound by memory.
+RV_HD inline int seq_share(int n, int x, int X) { return (int)((int64_t)n * x / X); }
+template <class A>
+RV_HD inline int seq_chunk_of(const A& a, int block) {
+  const int X = a.n_queues, x = block % X, rest = a.chunks - a.inner_chunks;
+  int j = block / X;
+  const int i0 = seq_share(a.inner_chunks, x, X), ni = seq_share(a.inner_chunks, x + 1, X) - i0;
+  if (j < ni) return i0 + j;
+  j -= ni;
+  const int l0 = seq_share(rest, x, X), nl = seq_share(rest, x + 1, X) - l0;
+  return j < nl ? a.inner_chunks + l0 + j : -1;
+}
+template <class A>
+RV_HD inline int seq_grid(const A& a) {
+  const int X = a.n_queues;
+  return X * ((a.inner_chunks + X - 1) / X + (a.chunks - a.inner_chunks + X - 1) / X);
+}
+
 // Partial slot of the segment of unit `unit` that chunk c takes, where c0 is the unit's first chunk.
 // Shared passes: a slot for each unit and chunk (their sum grows with each segment).  Other
 // units write partial results only where they are cut, and a unit of n chunks takes the n slots from

@@ -133,13 +133,16 @@ rv_status append(rv_pool p, int n, const int* seqs, const void* K, const void* V
     d.cow = old;
     d.page[0] = book.page(seqs[i], first);
     d.page[1] = first + 1 < end ? book.page(seqs[i], first + 1) : d.page[0];
-    d.fresh = (d.offset == 0 || old >= 0 ? 1 : 0) | (first + 1 < end ? 2 : 0);
+    // entries to write: of the first page where it is new or a copy, and of all after it
+    d.write0 = d.offset == 0 || old >= 0 ? 0 : 1;
+    d.in_a_row = book.in_a_row(seqs[i], first + 1) ? 1 : 0;
+    d.writes = (d.in_a_row ? end - first : std::min(end - first, 2)) - d.write0;
     d.n = r;
     d.src_row = src_row;
     src_row += r;
     const int64_t blocks = blocks_of((int64_t)(r + (old >= 0 ? d.offset : 0)) * p->n_heads);
     if (a.n_seqs == rv::kMaxAppend || a.blocks + blocks > rv::kMaxGridBlocks) flush();
-    for (int k = first + 2; k < end && err == hipSuccess; ++k)
+    for (int k = first + 2; !d.in_a_row && k < end && err == hipSuccess; ++k)
       err = runs.add(d.entry0 + (k - first), book.page(seqs[i], k), 1, false);
     d.block0 = a.blocks;
     a.blocks += (int)blocks;
@@ -388,9 +391,12 @@ rv_status rv_pool_compact(rv_pool p, int n, const int* seqs, const int64_t* firs
     keep0 += n_keep[i] * p->n_heads;
     const int64_t blocks = blocks_of((int64_t)(d.offset + d.n) * p->n_heads);
     if (a.n_seqs == rv::kMaxCompact || a.blocks + blocks > rv::kMaxGridBlocks) flush();
-    if (err == hipSuccess) err = runs.add(new0, d.old0, leading, true);
-    for (int k = leading; k < book.pages(seqs[i]) && err == hipSuccess; ++k)
-      err = runs.add(new0 + k, book.page(seqs[i], k), 1, false);
+    d.page0 = book.in_a_row(seqs[i], leading) ? book.page(seqs[i], leading) : -1;
+    if (d.page0 < 0) {
+      if (err == hipSuccess) err = runs.add(new0, d.old0, leading, true);
+      for (int k = leading; k < book.pages(seqs[i]) && err == hipSuccess; ++k)
+        err = runs.add(new0 + k, book.page(seqs[i], k), 1, false);
+    }
     d.block0 = a.blocks;
     a.blocks += (int)blocks;
     a.seq[a.n_seqs++] = d;

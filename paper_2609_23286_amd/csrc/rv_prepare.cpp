@@ -58,11 +58,11 @@ rv::PrepArgs base_args(const rv_qkv_prep& p, int n_tokens, const int32_t* pos) {
   return a;
 }
 
-// One token a wave while that leaves the device's waves unfilled, else more, so that a wave has
-// several rows in flight and its angles fill all lanes.
-void plan_waves(rv::PrepArgs* a, int n_cus, int max_blocks) {
-  const int64_t per = rv::ceil_div64(a->n_tokens, (int64_t)n_cus * 16);
-  a->tokens_per_wave = (int)std::min<int64_t>(rv::kPrepMaxTokens, std::max<int64_t>(1, per));
+// As many tokens a wave as fill its 16 rows of heads: more rows in a wave were slower than more waves
+// (8328 tokens of 16 heads: 27 us at three tokens a wave, 20 at one).
+void plan_waves(rv::PrepArgs* a, int max_blocks) {
+  const int heads = std::max(a->n_q_heads, a->n_kv_heads);
+  a->tokens_per_wave = std::min(rv::kPrepMaxTokens, std::max(1, 16 / heads));
   const int64_t blocks = rv::ceil_div64(a->n_tokens, (int64_t)a->tokens_per_wave * (rv::kPrepThreads / 64));
   a->blocks = (int)std::min<int64_t>(blocks, max_blocks);
 }
@@ -92,7 +92,7 @@ rv_status prepare(const rv_qkv_prep* p, const void* q, int64_t q_stride, const v
   a.V = (uint16_t*)V;
   a.kv_row = kv_row;
   a.kv_head = kv_head;
-  plan_waves(&a, ctx.n_cus, INT32_MAX);
+  plan_waves(&a, INT32_MAX);
   if (a.blocks > rv::kMaxGridBlocks) return fail(RV_ERR_INVALID, "too many tokens for one call");
   RV_HIP(rv::launch_prepare(a, dtype == RV_F32, p->n_axes, false, s), "prepare launch");
   return RV_OK;
@@ -177,7 +177,7 @@ rv_status rv_prepare_qkv_bwd(const rv_qkv_prep* p, const void* q, int64_t q_stri
   a.dkb = dk_bias;
   // a workgroup's sums are 256 floats; the workspace holds far more than two workgroups a CU need
   const int64_t room = (int64_t)(ctx.part_floats / (4 * rv::kHeadDim));
-  plan_waves(&a, ctx.n_cus, (int)std::min<int64_t>(2 * ctx.n_cus, room));
+  plan_waves(&a, (int)std::min<int64_t>(2 * ctx.n_cus, room));
   a.part = sums ? ctx.part : nullptr;
   RV_HIP(rv::launch_prepare(a, dtype == RV_F32, p->n_axes, true, (hipStream_t)stream), "prepare launch");
   return RV_OK;

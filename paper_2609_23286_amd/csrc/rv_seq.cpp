@@ -12,12 +12,15 @@
 namespace rv {
 
 void rotation_turns(double base, int n_freqs, uint64_t* out) {
+  // base^(-i / n) as the product of the powers at i's bits: six roundings of 64 bits at most
   const long double two_pi = 6.283185307179586476925286766559005768L;
+  long double bit[5];
+  for (int b = 0; b < 5; ++b) bit[b] = powl((long double)base, -(long double)(1 << b) / n_freqs);
   for (int i = 0; i < kMaxFreqs; ++i) {
-    out[i] = 0;
-    if (i >= n_freqs) continue;
-    const long double turns = powl((long double)base, -(long double)i / n_freqs) / two_pi;  // <= 0.16
-    out[i] = (uint64_t)(turns * 18446744073709551616.0L + 0.5L);
+    long double f = 1 / two_pi;  // (so the turns stay below 0.16)
+    for (int b = 0; b < 5; ++b)
+      if (i >> b & 1) f *= bit[b];
+    out[i] = i < n_freqs ? (uint64_t)(f * 18446744073709551616.0L + 0.5L) : 0;
   }
 }
 
@@ -101,7 +104,7 @@ void PageBook::fork(int child, int s, int64_t n_rows) {
 void PageBook::truncate(int s, int64_t n_rows) {
   const int have = pages(s);
   len_[s] = n_rows;
-  for (int i = pages(s); i < have; ++i) drop(page(s, i));
+  for (int i = have - 1; i >= pages(s); --i) drop(page(s, i));  // (so that they are taken in this order again)
 }
 
 bool PageBook::append_copies(int s, int64_t n) const {
@@ -124,6 +127,13 @@ int PageBook::append(int s, int64_t n) {
   }
   for (int i = have; i < pages(s); ++i) table_[entry0(s) + i] = take();
   return old;
+}
+
+bool PageBook::in_a_row(int s, int from) const {
+  const int32_t* x = list(s);
+  for (int i = from + 1, n = pages(s); i < n; ++i)
+    if (x[i] != x[i - 1] + 1) return false;
+  return true;
 }
 
 int PageBook::compact_pages(int64_t first, int64_t n_rows) const {
@@ -150,7 +160,7 @@ void PageBook::release_dropped() {
   while (n_moved_ > 0) {
     const int s = moved_[--n_moved_];
     const int32_t old = (2 * s + (side_[s] ^ 1)) * width_;
-    for (int i = 0; i < old_pages_[s]; ++i) drop(table_[old + i]);
+    for (int i = old_pages_[s] - 1; i >= 0; --i) drop(table_[old + i]);
   }
 }
 
@@ -175,7 +185,7 @@ int common_pages(const PageBook& book, int a, int b) {
 // for the narrow units and shortest chunks of 8 to 32 measured on twelve batches, from two single tokens to
 // 16 frames: these are within 4 % of the best of each but one, where narrow tiles of cost 1 and units of 20
 // are 5 % faster; without fixed shares long batches lost 10 to 40 %.)
-constexpr int kWideCost = 4, kWideFixed = 16, kNarrowCost = 2, kNarrowFixed = 12;
+constexpr int kWideCost = 4, kWideFixed = 16, kNarrowCost = 2, kNarrowFixed = 16;
 constexpr int kMinChunk = 20;     // positions
 // (no chunk between a unit's first and last is without a tile of it)
 static_assert(kMinChunk >= kWideFixed + kWideCost && kMinChunk >= kNarrowFixed + kNarrowCost, "chunk length");
@@ -195,7 +205,9 @@ struct Builder {
   bool overflow;
 
   int64_t tiles(int64_t n_tok) const { return ceil_div64(n_tok * group, tile_rows(n_tok)); }
-  int tile_rows(int64_t n_tok) const { return n_tok * group <= kSubRows ? kSubRows : kAttnBQ; }
+  int tile_rows(int64_t n_tok) const {
+    return n_tok * group <= kSubRows ? kSubRows : kAttnBQ;
+  }
 
   SeqPass make(int i, int j, int p0, int p1, int parent) const {
     SeqPass p{};
@@ -279,7 +291,7 @@ int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool 
     bool fits = true;
     for (int i = 0; i < a->n_pass; ++i) {
       SeqPass& p = a->pass[i];
-      const bool narrow = p.tile_rows == kSubRows;
+      const bool narrow = p.tile_rows < kAttnBQ;
       p.cost = narrow ? kNarrowCost : kWideCost;
       p.fixed = seq_tiles(p) == 0 ? 0 : narrow ? kNarrowFixed : kWideFixed;
       a->pos0[i] = p.pos0 = (int)std::min<int64_t>(pos, INT32_MAX);
@@ -290,10 +302,14 @@ int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool 
       continue;
     }
     // Chunks of equal length, one for each of the device's workgroup slots, but no shorter than
-    // kMinChunk.
+    // kMinChunk.  (With inner passes an XCD's two shares are rounded up each: a workgroup more than its
+    // slots would wait for a whole chunk.)
     a->total = (int)pos;
-    a->E = (int)std::max<int64_t>(kMinChunk, ceil_div64(pos, (int64_t)kAttnWgPerCu * n_cus));
+    const int slots_at_once = std::max(1, kAttnWgPerCu * n_cus - (a->n_inner > 0 ? a->n_queues : 0));
+    a->E = (int)std::max<int64_t>(kMinChunk, ceil_div64(pos, slots_at_once));
     a->chunks = (int)ceil_div64(pos, a->E);
+    const int leaf0 = a->n_inner < a->n_pass ? a->pass[a->n_inner].pos0 : a->total;
+    a->inner_chunks = (int)ceil_div64(leaf0, a->E);
     int64_t slots = (2 * (int64_t)a->chunks + 1) * kSubsPerTile, merge = 0;
     for (int i = 0; i < a->n_pass; ++i) {
       SeqPass& p = a->pass[i];

@@ -183,6 +183,33 @@ def _ptr_python(t, shape=None, itemsize=None, what="tensor"):
 _bind.setup(_ptr_python, ctypes.cast(_lib.rv_mem_view, ctypes.c_void_p).value,
             ctypes.cast(_lib.rv_mem_len, ctypes.c_void_p).value)
 _ptr, _ptrs = _bind.ptr, _bind.ptrs
+_bind.setup_calls(*(ctypes.cast(getattr(_lib, f), ctypes.c_void_p).value for f in (
+    "rv_prepare_qkv", "rv_prepare_qkv_bwd", "rv_pool_fork", "rv_pool_close", "rv_pool_append", "rv_pool_gather",
+    "rv_pool_compact", "rv_attend_seqs")))
+
+
+def _made(status):
+    """Whether a call made through _rv_bind went through; None: it was not made."""
+    if status is None:
+        return False
+    if status != RV_OK:
+        _check(status)
+    return True
+
+
+def _where(stream):
+    """(current device, stream handle) as integers."""
+    device = torch.cuda.current_device()
+    if stream is None and _raw_stream is not None:
+        return device, _raw_stream(device)
+    s = _stream(stream)
+    return device, s if isinstance(s, int) else s.value or 0
+
+
+def _same_device(device, *tensors):
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != device:
+            raise ValueError(f"a tensor on device {t.get_device()} while device {device} is current")
 
 
 def _mem_state(mem):
@@ -471,6 +498,7 @@ class QKVPrep:
         ptrs = [_ptr(t, (HEAD_DIM,), 4, "weight or bias") for t in self.vectors]
         self.c = rv_qkv_prep(n_q_heads, n_kv_heads, _NORMS[norm], axes, eps, base, *ptrs)
         self.n_q_heads, self.n_kv_heads, self.axes = n_q_heads, n_kv_heads, axes
+        self._args = (ctypes.addressof(self.c), axes, n_q_heads, n_kv_heads)
 
 
 def _rows(t, heads, what):
@@ -523,15 +551,20 @@ def _positions(prep, pos, n):
 def prepare_qkv(prep, q, k, v, pos, Q, K, V, stream=None):
     """rv_prepare_qkv: q [N, Hq * 64], k, v [N, Hk * 64] (bf16 or fp32, rows at any distance) to the frame
     tensors Q [N, Hq, 64], K, V [N, Hk, 64] bf16; pos [N, axes] int32.  v and V may be None."""
+    device, s = _where(stream)
+    if _made(_bind.prepare(*prep._args, device, s, q, k, v, pos, Q, K, V)):
+        return
+    _same_device(device, q, k, v, pos, Q, K, V, *prep.vectors)
     N, Hq, Hk = q.shape[0], prep.n_q_heads, prep.n_kv_heads
     src, dtype = _prep_rows(((q, Hq, "q"), (k, Hk, "k"), (v, Hk, "v")), N)
     _check(_lib.rv_prepare_qkv(ctypes.byref(prep.c), *src, dtype, N, _positions(prep, pos, N),
                                _ptr(Q, (N, Hq, HEAD_DIM), 2, "Q"), _ptr(K, (N, Hk, HEAD_DIM), 2, "K"),
-                               _ptr(V, (N, Hk, HEAD_DIM), 2, "V"), _stream(stream)))
+                               _ptr(V, (N, Hk, HEAD_DIM), 2, "V"), s))
 
 
 def stage_qkv(prep, q, k, v, pos, Q, mem, stream=None):
     """rv_mem_stage_qkv: prepare_qkv whose K and V become the frame staged in mem."""
+    _same_device(torch.cuda.current_device(), q, k, v, pos, Q, *prep.vectors)
     N, Hq, Hk = q.shape[0], prep.n_q_heads, prep.n_kv_heads
     src, dtype = _prep_rows(((q, Hq, "q"), (k, Hk, "k"), (v, Hk, "v")), N)
     _check(_lib.rv_mem_stage_qkv(mem.handle, ctypes.byref(prep.c), *src, dtype, N, _positions(prep, pos, N),
@@ -543,6 +576,11 @@ def prepare_qkv_bwd(prep, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight=None, dq_
     """rv_prepare_qkv_bwd: the gradients dq, dk, dv of prepare_qkv's inputs (their dtype, rows at any
     distance) and, where given, of the weights and biases ([64] fp32, overwritten), from dQ [N, Hq, 64]
     and dK, dV [N, Hk, 64] bf16.  dV and dv may be None."""
+    device, s = _where(stream)
+    if _made(_bind.prepare_bwd(*prep._args, device, s, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight, dq_bias,
+                               dk_weight, dk_bias)):
+        return
+    _same_device(device, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight, dq_bias, dk_weight, dk_bias, *prep.vectors)
     N, Hq, Hk = q.shape[0], prep.n_q_heads, prep.n_kv_heads
     rows, dtype = _prep_rows(((q, Hq, "q"), (k, Hk, "k"), (dq, Hq, "dq"), (dk, Hk, "dk"), (dv, Hk, "dv")), N)
     sums = []
@@ -552,7 +590,7 @@ def prepare_qkv_bwd(prep, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight=None, dq_
         sums.append(_ptr(t, (HEAD_DIM,), 4, name))
     _check(_lib.rv_prepare_qkv_bwd(ctypes.byref(prep.c), *rows[:4], dtype, N, _positions(prep, pos, N),
                                    _ptr(dQ, (N, Hq, HEAD_DIM), 2, "dQ"), _ptr(dK, (N, Hk, HEAD_DIM), 2, "dK"),
-                                   _ptr(dV, (N, Hk, HEAD_DIM), 2, "dV"), *rows[4:], *sums, _stream(stream)))
+                                   _ptr(dV, (N, Hk, HEAD_DIM), 2, "dV"), *rows[4:], *sums, s))
 
 
 # ---- sequences in pages ----------------------------------------------------------------
@@ -578,6 +616,10 @@ class Pool:
         _check(_lib.rv_pool_create(n_heads, head_dim, n_pages, max_seqs, max_rows, ctypes.byref(h)))
         self.handle = h
         self.n_heads = n_heads
+
+    @property
+    def _address(self):
+        return self.handle.value if self.handle else 0
 
     def close(self):
         if self.handle:
@@ -606,13 +648,20 @@ class Pool:
 
     def fork(self, seq, n_rows=None, n=1, stream=None):
         """rv_pool_fork: a list of n new sequences that share the first n_rows rows (default: all)."""
-        out = (ctypes.c_int * n)()
         rows = self.len(seq) if n_rows is None else n_rows
-        _check(_lib.rv_pool_fork(self.handle, seq, rows, n, out, _stream(stream)))
+        s = _where(stream)[1]
+        out = _bind.fork(self._address, s, seq, rows, n)
+        if isinstance(out, list):
+            return out
+        if not _made(out):
+            out = (ctypes.c_int * n)()
+            _check(_lib.rv_pool_fork(self.handle, seq, rows, n, out, s))
         return list(out)
 
     def release(self, seqs):
         """rv_pool_close: close sequences; pages without another user are free."""
+        if _made(_bind.release(self._address, seqs)):
+            return
         _check(_lib.rv_pool_close(self.handle, len(seqs), _ints(seqs, len(seqs), "seqs")))
 
     def truncate(self, seq, n_rows):
@@ -621,14 +670,22 @@ class Pool:
 
     def append(self, seqs, K, V, n_rows, stream=None):
         """rv_pool_append: n_rows[i] rows of K, V [sum of n_rows, H, 64] to seqs[i]."""
+        device, s = _where(stream)
+        if _made(_bind.append(self._address, self.n_heads, device, s, seqs, K, V, n_rows)):
+            return
+        _same_device(device, K, V)
         n = len(seqs)
         shp = (sum(n_rows), self.n_heads, HEAD_DIM)
         _check(_lib.rv_pool_append(self.handle, n, _ints(seqs, n, "seqs"), _ptr(K, shp, 2, "K"), _ptr(V, shp, 2, "V"),
-                                   _ints(n_rows, n, "n_rows"), _stream(stream)))
+                                   _ints(n_rows, n, "n_rows"), s))
 
     def gather(self, seqs, K, V, n_rows, first=None, stream=None):
         """rv_pool_gather: rows first[i] (default 0) .. + n_rows[i] of seqs[i] to the next [H, n_rows[i], 64] of K
         and V (contiguous, sum of n_rows * H rows in all; either may be None)."""
+        device, s = _where(stream)
+        if _made(_bind.gather(self._address, self.n_heads, device, s, seqs, n_rows, first, K, V)):
+            return
+        _same_device(device, K, V)
         n, size = len(seqs), sum(n_rows) * self.n_heads * HEAD_DIM
         for t, what in ((K, "K"), (V, "V")):
             if t is not None and t.numel() != size:
@@ -636,24 +693,31 @@ class Pool:
         _check(_lib.rv_pool_gather(
             self.handle, n, _ints(seqs, n, "seqs"), _ints(first, n, "first", ctypes.c_int64),
             _ints(n_rows, n, "n_rows", ctypes.c_int64), K if K is None else _ptr(K, tuple(K.shape), 2, "K"),
-            V if V is None else _ptr(V, tuple(V.shape), 2, "V"), _stream(stream)))
+            V if V is None else _ptr(V, tuple(V.shape), 2, "V"), s))
 
     def compact(self, seqs, keep, n_keep, first=None, stream=None):
         """rv_pool_compact: seqs[i] keeps its rows before first[i] (default 0) and the n_keep[i] rows of each
         head that keep (int32, [H, n_keep[i]] for each i in turn) names."""
+        device, s = _where(stream)
+        if _made(_bind.compact(self._address, self.n_heads, device, s, seqs, n_keep, first, keep)):
+            return
+        _same_device(device, keep)
         n, size = len(seqs), sum(n_keep) * self.n_heads
         if keep is not None and (keep.numel() != size or keep.dtype != torch.int32):
             raise ValueError(f"keep: {keep.numel()} values of {keep.dtype}, expected {size} of torch.int32")
         _check(_lib.rv_pool_compact(self.handle, n, _ints(seqs, n, "seqs"), _ints(first, n, "first", ctypes.c_int64),
                                     _ints(n_keep, n, "n_keep", ctypes.c_int64),
-                                    keep if keep is None else _ptr(keep, tuple(keep.shape), 4, "keep"),
-                                    _stream(stream)))
+                                    keep if keep is None else _ptr(keep, tuple(keep.shape), 4, "keep"), s))
 
 
 def attend_seqs(Q, K, V, pool, seqs, n_tokens, out, lse, stream=None):
     """rv_attend_seqs: the queries of several sequences, Q, out [sum of n_tokens, Hq, 64] bf16, over the
     sequences' rows and (unless None) their own keys K, V [sum of n_tokens, H, 64]; lse: fp32,
     [Hq, n_tokens[i]] for each i in turn ([n, Hq, N] where all have N tokens)."""
+    device, s = _where(stream)
+    if _made(_bind.attend(pool._address, pool.n_heads, device, s, seqs, n_tokens, Q, K, V, out, lse)):
+        return
+    _same_device(device, Q, K, V, out, lse)
     n, total = len(seqs), sum(n_tokens)
     Hq = Q.shape[1]
     shp, kv = (total, Hq, HEAD_DIM), (total, pool.n_heads, HEAD_DIM)
@@ -661,12 +725,13 @@ def attend_seqs(Q, K, V, pool, seqs, n_tokens, out, lse, stream=None):
         raise ValueError(f"lse: {lse.numel()} elements, expected {total * Hq}")
     _check(_lib.rv_attend_seqs(pool.handle, n, _ints(seqs, n, "seqs"), _ints(n_tokens, n, "n_tokens"),
                                _ptr(Q, shp, 2, "Q"), _ptr(K, kv, 2, "K"), _ptr(V, kv, 2, "V"), Hq,
-                               _ptr(out, shp, 2, "out"), _ptr(lse, tuple(lse.shape), 4, "lse"), _stream(stream)))
+                               _ptr(out, shp, 2, "out"), _ptr(lse, tuple(lse.shape), 4, "lse"), s))
 
 
 def admit_seqs(Q, K, V, lse, qs, budget, pool, seqs, saliency_out, idx_out, stream=None):
     """rv_admit_seqs: each frame's `budget` most salient rows per head to its sequence.  Q, K, V
     [n, N, H, 64] bf16; lse, saliency_out [n, H, N] fp32; idx_out [n, H, budget] int32."""
+    _same_device(torch.cuda.current_device(), Q, K, V, lse, saliency_out, idx_out)
     n, N, H, d = Q.shape
     if (n, H) != (len(seqs), pool.n_heads):
         raise ValueError(f"Q: {n} frames of {H} heads for {len(seqs)} sequences of {pool.n_heads} heads")

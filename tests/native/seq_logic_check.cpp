@@ -83,6 +83,9 @@ struct World {
       const int before = book.free_pages(), want = book.append_pages(seqs[i], n[i]);
       const int old = book.append(seqs[i], n[i]);
       CHECK(before - book.free_pages() == want, "pages taken");
+      bool row = true;
+      for (int k = 1; k < book.pages(seqs[i]); ++k) row = row && book.page(seqs[i], k) == book.page(seqs[i], k - 1) + 1;
+      CHECK(book.in_a_row(seqs[i], 0) == row, "pages in a row");
       if (old >= 0) copies.push_back({old, book.page(seqs[i], start / 64), (int)(start % 64)});
       for (int k = 0; k < n[i]; ++k) {
         const int64_t r = start + k;
@@ -148,6 +151,7 @@ struct World {
     const int64_t max_slots = uniform(0, 3) ? 8192 : 300;
     for (size_t i = 0; i < span.size();) {
       rv::SeqArgs a{};
+      a.n_queues = uniform(1, 9);
       const int done = rv::plan_seqs(book, &span[i], (int)(span.size() - i), tok0, frame, n_heads, group,
                                      uniform(1, 300), max_slots, &a);
       CHECK(done >= 1 && done <= (int)(span.size() - i), "sequences covered");
@@ -162,7 +166,14 @@ struct World {
         while (i + 1 < a.n_pass && a.pass[i + 1].pos0 <= x) ++i;
         return i;
       };
-      for (int c = 0; c < a.chunks; ++c) {
+      std::vector<int> order;
+      for (int b = 0; b < rv::seq_grid(a); ++b)
+        if (rv::seq_chunk_of(a, b) >= 0) order.push_back(rv::seq_chunk_of(a, b));
+      std::vector<int> sorted = order;
+      std::sort(sorted.begin(), sorted.end());
+      for (int c = 0; c < a.chunks; ++c) CHECK(c < (int)sorted.size() && sorted[c] == c, "chunk %d", c);
+      CHECK((int)sorted.size() == a.chunks, "chunks taken");
+      for (int c : order) {
         const int begin = c * a.E, end = std::min(begin + a.E, a.total);
         int ip = last_below(begin);
         for (int pos = begin; pos < end;) {
