@@ -1,12 +1,16 @@
 // prepare.hip -- projection outputs to frame tensors, gfx950: the norm of every query and key
 // head and the rotation by the token's position, and their gradients.
 //
-// Layout.  Four lanes hold a head's 64 elements, 16 each, as two 8-element chunks a and b that
-// are the rotation's two halves: with two axes lane j holds chunks {0,1,4,5}[j] and the chunk two
-// further on, with one axis (and none) chunks j and j + 4.  So a pair's two elements lie in one
-// lane, the norm's sums are 16 adds and two exchanges in a quad, and 16 heads fill a wave.  A wave
-// takes `tokens_per_wave` consecutive tokens: their heads are one list of rows (token, head), 16 to
-// an iteration, queries first, then keys; the values are copied.
+// Layout.  Eight lanes hold a head's 64 elements, 8 each, as two pieces of 4, chosen so that every
+// access is 16 bytes a lane and whole lines a row: of bf16 rows a lane's pieces are neighbours, of fp32 rows
+// (128 bytes to an instruction) 32 elements apart.  The partner of an element in its rotation pair
+// lies in lane j ^ 2 (with fp32 rows and one axis: in the lane itself); where that needs it, the lane
+// number's bits 1 and 2 change places.  The multiply-add reads the partner through a lane exchange, and the
+// norm's sums are 8 adds and three exchanges.  Eight heads fill a wave.  A wave takes a token (or a few, where
+// they have fewer than eight heads): its rows (token, head) of queries, of keys and of values are requested at
+// once, eight to an instruction.  Few registers are held per lane, so that the waves a CU holds cover the
+// latency of memory, which bounds it.  Results are written past the caches' reuse (nontemporal: 8328 tokens of
+// 16 heads 24.5 -> 19.6 us, 5.2 TB/s; the attention that follows takes the same time).
 //
 // Angles.  A token's position gives 32 distinct (axis, frequency) pairs whatever its head count, so
 // each lane of the wave forms one pair's sine and cosine and the heads read them from LDS.  The
@@ -21,11 +25,9 @@ namespace {
 constexpr int D = kHeadDim;
 constexpr int NT = kPrepThreads;
 constexpr int NW = NT / 64;
-constexpr int kAngles = kMaxFreqs;  // per token: axes x frequencies
-
-struct Pair16 {   // a lane's 16 elements: a[i] and b[i] turn together
-  float a[8], b[8];
-};
+constexpr int E = 8;               // elements a lane
+constexpr int R = 64 * E / D;      // rows (heads) a wave takes at a time
+static_assert(R == kPrepRows, "the host sizes a wave's tokens by it");
 
 // x = 2 pi phase / 2^32 within an eighth of a turn, by the Taylor series of sine (to x^9, the next
 // term is below 2^-29) and cosine (to x^10, 2^-32), and the quadrant's exchange and signs.
@@ -39,256 +41,310 @@ __device__ __forceinline__ float2 sin_cos_turns(uint32_t phase) {
   return make_float2((quad & 2) ? -sv : sv, ((quad + 1) & 2) ? -cv : cv);
 }
 
-template <bool F32>
-__device__ __forceinline__ void store8(void* base, int64_t at, const float (&x)[8]) {
-  if (F32) {
-    float4* p = reinterpret_cast<float4*>(static_cast<float*>(base) + at);
-    p[0] = make_float4(x[0], x[1], x[2], x[3]);
-    p[1] = make_float4(x[4], x[5], x[6], x[7]);
-  } else {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    const bf16x2 p0 = {(__bf16)x[0], (__bf16)x[1]}, p1 = {(__bf16)x[2], (__bf16)x[3]};
-    const bf16x2 p2 = {(__bf16)x[4], (__bf16)x[5]}, p3 = {(__bf16)x[6], (__bf16)x[7]};
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + at) =
-        make_uint4(__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1), __builtin_bit_cast(uint32_t, p2),
-                   __builtin_bit_cast(uint32_t, p3));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Where a lane's two pieces of 4 elements lie in a head (WIDE: the rows that count are fp32).
+template <bool WIDE>
+struct Cols {
+  int a, b;
+};
+template <bool WIDE, int AXES>
+__device__ __forceinline__ Cols<WIDE> lane_cols(int lane) {
+  const int j = lane & 7, turned = (j & 1) | (j & 2) << 1 | (j & 4) >> 1;
+  if (WIDE) {
+    const int c = AXES == 2 ? turned : j;
+    return {4 * c, D / 2 + 4 * c};
   }
+  const int c = AXES == 1 ? turned : j;
+  return {E * c, E * c + 4};
 }
 
-// A lane's 16 elements as they are in memory, so that loads can be issued well before their use.
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// A lane's 8 elements as they are in memory, so that loads can be issued well before their use.
 template <bool F32>
-struct Raw16 {
-  u32x4 a0, b0, a1, b1;  // (the second pair: fp32)
+struct Raw {
+  u32x4 lo, hi;  // (hi: fp32)
 };
-
-template <bool F32>
-__device__ __forceinline__ Raw16<F32> load_raw(const void* base, int64_t at, int a, int b) {
-  constexpr int S = F32 ? 4 : 2;
-  const char* p = static_cast<const char*>(base) + at * S;
-  Raw16<F32> r;
-  r.a0 = *reinterpret_cast<const u32x4*>(p + a * S);
-  r.b0 = *reinterpret_cast<const u32x4*>(p + b * S);
+template <bool F32, bool WIDE>
+__device__ __forceinline__ Raw<F32> load_raw(const void* base, int64_t at, Cols<WIDE> c) {
+  const char* p = static_cast<const char*>(base) + at * (F32 ? 4 : 2);
+  Raw<F32> r;
   if (F32) {
-    r.a1 = *reinterpret_cast<const u32x4*>(p + a * S + 16);
-    r.b1 = *reinterpret_cast<const u32x4*>(p + b * S + 16);
+    r.lo = *reinterpret_cast<const u32x4*>(p + c.a * 4);
+    r.hi = *reinterpret_cast<const u32x4*>(p + c.b * 4);
+  } else if (WIDE) {
+    const u32x2 x = *reinterpret_cast<const u32x2*>(p + c.a * 2), y = *reinterpret_cast<const u32x2*>(p + c.b * 2);
+    r.lo = u32x4{x[0], x[1], y[0], y[1]};
+  } else {
+    r.lo = *reinterpret_cast<const u32x4*>(p + c.a * 2);
   }
   return r;
 }
-
 template <bool F32>
-__device__ __forceinline__ void unpack(const Raw16<F32>& r, Pair16& x) {
+__device__ __forceinline__ void unpack(const Raw<F32>& r, float (&x)[E]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (F32) {
-      x.a[i] = __uint_as_float(r.a0[i]), x.a[4 + i] = __uint_as_float(r.a1[i]);
-      x.b[i] = __uint_as_float(r.b0[i]), x.b[4 + i] = __uint_as_float(r.b1[i]);
+      x[i] = __uint_as_float(r.lo[i]), x[4 + i] = __uint_as_float(r.hi[i]);
     } else {
-      x.a[2 * i] = __uint_as_float(r.a0[i] << 16), x.a[2 * i + 1] = __uint_as_float(r.a0[i] & 0xFFFF0000u);
-      x.b[2 * i] = __uint_as_float(r.b0[i] << 16), x.b[2 * i + 1] = __uint_as_float(r.b0[i] & 0xFFFF0000u);
+      x[2 * i] = __uint_as_float(r.lo[i] << 16), x[2 * i + 1] = __uint_as_float(r.lo[i] & 0xFFFF0000u);
     }
+  }
+}
+
+template <bool F32, bool WIDE>
+__device__ __forceinline__ void store8(void* base, int64_t at, Cols<WIDE> c, const float (&x)[E]) {
+  if (F32) {
+    float* p = static_cast<float*>(base) + at;
+    __builtin_nontemporal_store((f32x4{x[0], x[1], x[2], x[3]}), reinterpret_cast<f32x4*>(p + c.a));
+    __builtin_nontemporal_store((f32x4{x[4], x[5], x[6], x[7]}), reinterpret_cast<f32x4*>(p + c.b));
+    return;
+  }
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 p0 = {(__bf16)x[0], (__bf16)x[1]}, p1 = {(__bf16)x[2], (__bf16)x[3]};
+  const bf16x2 p2 = {(__bf16)x[4], (__bf16)x[5]}, p3 = {(__bf16)x[6], (__bf16)x[7]};
+  const u32x4 v = {__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1), __builtin_bit_cast(uint32_t, p2),
+                   __builtin_bit_cast(uint32_t, p3)};
+  uint16_t* p = static_cast<uint16_t*>(base) + at;
+  if (WIDE) {
+    __builtin_nontemporal_store((u32x2{v[0], v[1]}), reinterpret_cast<u32x2*>(p + c.a));
+    __builtin_nontemporal_store((u32x2{v[2], v[3]}), reinterpret_cast<u32x2*>(p + c.b));
+  } else {
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p + c.a));
   }
 }
 
 template <int CTRL>
-__device__ __forceinline__ float quad_add(float x) {
-  return x + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true));
+__device__ __forceinline__ float from_lane(float x) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true));
 }
-// Sum over the four lanes of a head.
-__device__ __forceinline__ float head_sum(float x) { return quad_add<0x4E>(quad_add<0xB1>(x)); }
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E;  // lanes exchanged within a quad
+constexpr int kMirror8 = 0x141;            // lane 7 - j of the eight
+constexpr int kRotate8 = 0x128;            // the lane 8 away, of 16
+// Sum over the eight lanes of a row.
+__device__ __forceinline__ float row_sum(float x) {
+  x += from_lane<kXor1>(x);
+  x += from_lane<kXor2>(x);
+  return x + from_lane<kMirror8>(x);
+}
 
-// The angles of tokens t0 .. t0 + n - 1, into the wave's table: [token][axis][frequency].
+// The angles of tokens t0 .. t0 + n - 1, into the wave's table: [token][element] (sine, cosine), the sine
+// with the sign its element's partner takes it with.  A lane forms items lane, lane + 64, ...; the position of
+// the first is loaded ahead (loads return in order: behind the rows' loads it would wait for them).
 template <int AXES>
-__device__ __forceinline__ void fill_angles(const PrepArgs& a, int t0, int n, int lane, float2* table) {
-  constexpr int per_axis = AXES == 2 ? 16 : 32;
-  for (int i = lane; i < n * kAngles; i += 64) {
-    const int t = i / kAngles, axis = AXES == 2 ? (i % kAngles) / per_axis : 0;
-    const int64_t pos = a.pos[(int64_t)(t0 + t) * AXES + axis];
-    table[i] = sin_cos_turns((uint32_t)(((uint64_t)pos * a.freq[i % per_axis]) >> 32));
+struct Angles {
+  static constexpr int kBlock = D / (AXES > 0 ? AXES : 1), kFreqs = kBlock / 2;
+  int32_t first = 0;
+  __device__ __forceinline__ int32_t position(const PrepArgs& a, int t0, int i) const {
+    return a.pos[(int64_t)(t0 + i / kMaxFreqs) * AXES + i % kMaxFreqs / kFreqs];
   }
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
-// Where a lane's two chunks lie, and its angles in a token's table.
-template <int AXES>
-struct LaneMap {
-  int a, b, angle;
-  __device__ explicit LaneMap(int j) {
-    a = 8 * (AXES == 2 ? (j & 1) + 4 * (j >> 1) : j);
-    b = a + (AXES == 2 ? 16 : 32);
-    angle = 8 * j;  // two axes: axis j / 2, frequencies 8 (j % 2) ..; one: frequencies 8 j ..
+  __device__ __forceinline__ void start(const PrepArgs& a, int t0, int n, int lane) {
+    if (AXES > 0 && lane < n * kMaxFreqs) first = position(a, t0, lane);
+  }
+  __device__ __forceinline__ void fill(const PrepArgs& a, int t0, int n, int lane, float2* table) {
+    if (AXES == 0) return;
+    for (int i = lane; i < n * kMaxFreqs; i += 64) {
+      const int64_t pos = i == lane ? first : position(a, t0, i);
+      const int f = i % kFreqs;
+      const float2 sc = sin_cos_turns((uint32_t)(((uint64_t)pos * a.freq[f]) >> 32));
+      float2* const e = table + i / kMaxFreqs * D + i % kMaxFreqs / kFreqs * kBlock + f;
+      e[0] = make_float2(-sc.x, sc.y);
+      e[kFreqs] = sc;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   }
 };
 
-// Turns every pair by its angle (backward: by minus its angle).
-template <int AXES, bool BACK>
-__device__ __forceinline__ void rotate(const float2* angles, Pair16& x) {
+// Turns every pair by its angle (BACK: by minus its angle).
+template <bool WIDE, int AXES, bool BACK>
+__device__ __forceinline__ void rotate(const float2* angles, Cols<WIDE> c, float (&x)[E]) {
   if (AXES == 0) return;
+  float y[E];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float2 sc = angles[i];
-    const float s = BACK ? -sc.x : sc.x, p = x.a[i], q = x.b[i];
-    x.a[i] = p * sc.y - q * s;
-    x.b[i] = q * sc.y + p * s;
+  for (int i = 0; i < E; ++i) y[i] = WIDE && AXES == 1 ? x[i ^ 4] : from_lane<kXor2>(x[i]);
+#pragma unroll
+  for (int i = 0; i < E; i += 2) {
+    const float4 sc = *reinterpret_cast<const float4*>(angles + (i < 4 ? c.a : c.b) + (i & 3));
+    x[i] = x[i] * sc.y + y[i] * (BACK ? -sc.x : sc.x);
+    x[i + 1] = x[i + 1] * sc.w + y[i + 1] * (BACK ? -sc.z : sc.z);
   }
 }
 
 // x to its normed form g r; returns r.
-__device__ __forceinline__ float normalise(int norm, float eps, Pair16& x) {
+__device__ __forceinline__ float normalise(int norm, float eps, float (&x)[E]) {
   if (norm == RV_NORM_LAYER) {
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += x.a[i] + x.b[i];
-    const float mean = head_sum(s) * (1.f / D);
+    for (int i = 0; i < E; ++i) s += x[i];
+    const float mean = row_sum(s) * (1.f / D);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x.a[i] -= mean, x.b[i] -= mean;
+    for (int i = 0; i < E; ++i) x[i] -= mean;
   }
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) s = fmaf(x.a[i], x.a[i], fmaf(x.b[i], x.b[i], s));
-  const float r = 1.f / sqrtf(head_sum(s) * (1.f / D) + eps);
+  for (int i = 0; i < E; ++i) s = fmaf(x[i], x[i], s);
+  const float r = 1.f / sqrtf(row_sum(s) * (1.f / D) + eps);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x.a[i] *= r, x.b[i] *= r;
+  for (int i = 0; i < E; ++i) x[i] *= r;
   return r;
 }
 
-// A weight or bias vector's elements at the lane's chunks; the default where there is none (by address: a branch
-// around the loads would wait for them).
+// The weights and biases, q w, q b, k w, k b, in LDS (a load of them among the rows' would wait for those):
+// thread i holds element i % 64 of vector i / 64.  The default stands in for one that there is not, by its address.
 __device__ const float kOnes[D] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1,
                                    1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1,
                                    1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1};
 __device__ const float kZeros[D] = {};
-__device__ __forceinline__ void load_vec(const float* p, const float* dflt, int a, int b, Pair16& x) {
-  unpack(load_raw<true>(p ? p : dflt, 0, a, b), x);
+__device__ __forceinline__ float own_weight(const PrepArgs& a) {
+  const int v = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const float* p = v == 0 ? a.qw : v == 1 ? a.qb : v == 2 ? a.kw : a.kb;
+  if (!p) p = v & 1 ? kZeros : kOnes;
+  return p[threadIdx.x & 63];
+}
+template <bool WIDE>
+__device__ __forceinline__ void read_vec(const float* vec, Cols<WIDE> c, float (&x)[E]) {
+  const float4 lo = *reinterpret_cast<const float4*>(vec + c.a), hi = *reinterpret_cast<const float4*>(vec + c.b);
+  x[0] = lo.x, x[1] = lo.y, x[2] = lo.z, x[3] = lo.w, x[4] = hi.x, x[5] = hi.y, x[6] = hi.z, x[7] = hi.w;
 }
 
-// One part (queries or keys) of the forward pass: rows r, r + 16, ... of n * H, the first already loaded; the
-// next row's elements are requested before this one's are worked on.
-template <bool F32, int AXES>
-__device__ __forceinline__ void prepare_part(const PrepArgs& a, const LaneMap<AXES>& m, const float2* angles, int t0, int n,
-                                             int lane, int H, const void* src, int64_t stride, uint16_t* dst, int64_t dst_row,
-                                             int64_t dst_head, const float* weight, const float* bias_p, Raw16<F32> raw) {
-  Pair16 w, bias;
-  if (a.norm != RV_NORM_NONE) {
-    load_vec(weight, kOnes, m.a, m.b, w);
-    load_vec(bias_p, kZeros, m.a, m.b, bias);
+// The rows of one part (queries, keys or values) of a wave's tokens: row r is head r % H of token t0 + r / H.
+// ONE: a wave has a single token (its rows then lie at a scalar base).
+template <bool ONE>
+struct Rows {
+  int t0, n, H;
+  __device__ __forceinline__ int count() const { return ONE ? H : n * H; }
+  __device__ __forceinline__ int token(int r) const { return ONE ? 0 : r / H; }
+  // element offset of row r where tokens are `row` elements apart and heads `head`
+  __device__ __forceinline__ int64_t at(int r, int64_t row, int64_t head) const {
+    if (ONE) return t0 * row + r * head;
+    const int t = token(r);
+    return (int64_t)(t0 + t) * row + (r - t * H) * head;
   }
-  for (int r = lane >> 2; r < n * H; r += 16) {
-    const int t = n == 1 ? 0 : r / H, h = r - t * H;
-    Pair16 x;
-    unpack(raw, x);
-    if (r + 16 < n * H) {
-      const int t2 = n == 1 ? 0 : (r + 16) / H, h2 = r + 16 - t2 * H;
-      raw = load_raw<F32>(src, (int64_t)(t0 + t2) * stride + h2 * D, m.a, m.b);
-    }
+};
+
+// The first rows of a part, kFirst to a lane, requested together; later ones as the earlier are done.
+constexpr int kFirst = 2;
+template <bool F32, bool WIDE, bool ONE>
+struct Ahead {
+  Raw<F32> raw[kFirst];
+  __device__ __forceinline__ void start(const void* src, const Rows<ONE>& p, int r, int64_t row, int64_t head, Cols<WIDE> c) {
+#pragma unroll
+    for (int k = 0; k < kFirst; ++k)
+      if (r + k * R < p.count()) raw[k] = load_raw<F32, WIDE>(src, p.at(r + k * R, row, head), c);
+  }
+  // Row r's elements; row r + kFirst R takes their place.
+  __device__ __forceinline__ void next(const void* src, const Rows<ONE>& p, int r, int64_t row, int64_t head,
+                                       Cols<WIDE> c, float (&x)[E]) {
+    unpack(raw[0], x);
+#pragma unroll
+    for (int k = 0; k + 1 < kFirst; ++k) raw[k] = raw[k + 1];
+    if (r + kFirst * R < p.count()) raw[kFirst - 1] = load_raw<F32, WIDE>(src, p.at(r + kFirst * R, row, head), c);
+  }
+};
+
+template <bool F32, int AXES, bool ONE>
+__device__ __forceinline__ void prepare_part(const PrepArgs& a, const Rows<ONE>& p, const float2* angles, int lane, const void* src,
+                                             int64_t stride, uint16_t* dst, int64_t dst_row, int64_t dst_head,
+                                             const float* vecs, Ahead<F32, F32, ONE>& ahead) {
+  const Cols<F32> c = lane_cols<F32, AXES>(lane);
+  for (int r = lane / 8; r < p.count(); r += R) {
+    float x[E];
+    ahead.next(src, p, r, stride, D, c, x);
     if (a.norm != RV_NORM_NONE) {
+      float w[E], b[E];
+      read_vec(vecs, c, w);
+      read_vec(vecs + D, c, b);
       normalise(a.norm, a.eps, x);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x.a[i] = fmaf(x.a[i], w.a[i], bias.a[i]);
-        x.b[i] = fmaf(x.b[i], w.b[i], bias.b[i]);
-      }
+      for (int i = 0; i < E; ++i) x[i] = fmaf(x[i], w[i], b[i]);
     }
-    rotate<AXES, false>(angles + t * kAngles + m.angle, x);
-    const int64_t to = (int64_t)(t0 + t) * dst_row + h * dst_head;
-    store8<false>(dst, to + m.a, x.a);
-    store8<false>(dst, to + m.b, x.b);
+    rotate<F32, AXES, false>(angles + p.token(r) * D, c, x);
+    store8<false, F32>(dst, p.at(r, dst_row, dst_head), c, x);
   }
 }
 
-template <bool F32, int AXES>
+template <bool F32, int AXES, bool ONE>
 __global__ __launch_bounds__(NT) void prepare_kernel(PrepArgs a) {
-  __shared__ float2 s_angles[NW][kPrepMaxTokens * kAngles];
+  __shared__ __attribute__((aligned(16))) float2 s_angles[NW][kPrepMaxTokens * D];
+  __shared__ __attribute__((aligned(16))) float s_vec[4 * D];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t first = ((int64_t)blockIdx.x * NW + wave) * a.tokens_per_wave;
-  if (first >= a.n_tokens) return;  // uniform in the wave; no barrier follows
-  const int t0 = (int)first, n = min(a.tokens_per_wave, a.n_tokens - t0);
+  const int t0 = (int)min(first, (int64_t)a.n_tokens), n = min(a.tokens_per_wave, a.n_tokens - t0);  // n: 0 past the end
+  const Cols<F32> c = lane_cols<F32, AXES>(lane);
+  const int r = lane / 8;
   float2* const angles = s_angles[wave];
-  const LaneMap<AXES> m(lane & 3);
-  // The first rows of all three parts are requested at once, before anything waits.
-  const int Hq = a.n_q_heads, Hk = a.n_kv_heads, r = lane >> 2;
-  const int tq = n == 1 ? 0 : r / Hq, tk = n == 1 ? 0 : r / Hk;
-  Raw16<F32> q{}, k{};
-  if (r < n * Hq) q = load_raw<F32>(a.q, (int64_t)(t0 + tq) * a.q_stride + (r - tq * Hq) * D, m.a, m.b);
-  if (r < n * Hk) k = load_raw<F32>(a.k, (int64_t)(t0 + tk) * a.k_stride + (r - tk * Hk) * D, m.a, m.b);
-  if (a.V) {  // (values in the same pattern: a lane's two chunks of a row)
-    Raw16<F32> v{};
-    if (r < n * Hk) v = load_raw<F32>(a.v, (int64_t)(t0 + tk) * a.v_stride + (r - tk * Hk) * D, m.a, m.b);
-    if (AXES > 0) fill_angles<AXES>(a, t0, n, lane, angles);
-    for (int i = r; i < n * Hk; i += 16) {
-      const int t = n == 1 ? 0 : i / Hk, h = i - t * Hk;
-      Pair16 x;
-      unpack(v, x);
-      if (i + 16 < n * Hk) {
-        const int t2 = n == 1 ? 0 : (i + 16) / Hk, h2 = i + 16 - t2 * Hk;
-        v = load_raw<F32>(a.v, (int64_t)(t0 + t2) * a.v_stride + h2 * D, m.a, m.b);
-      }
-      const int64_t to = (int64_t)(t0 + t) * a.kv_row + h * a.kv_head;
-      store8<false>(a.V, to + m.a, x.a);
-      store8<false>(a.V, to + m.b, x.b);
-    }
-  } else if (AXES > 0) {
-    fill_angles<AXES>(a, t0, n, lane, angles);
+  const Rows<ONE> pq{t0, n, a.n_q_heads}, pk{t0, n, a.n_kv_heads};
+  const bool norm = a.norm != RV_NORM_NONE;
+  Angles<AXES> ang;
+  Ahead<F32, F32, ONE> q, k, v;
+  float vec = 0.f;
+  if (norm) vec = own_weight(a);
+  if (n > 0) {
+    ang.start(a, t0, n, lane);
+    q.start(a.q, pq, r, a.q_stride, D, c);
+    k.start(a.k, pk, r, a.k_stride, D, c);
+    if (a.V) v.start(a.v, pk, r, a.v_stride, D, c);
   }
-  prepare_part<F32, AXES>(a, m, angles, t0, n, lane, Hq, a.q, a.q_stride, a.Q, (int64_t)Hq * D, D, a.qw, a.qb, q);
-  prepare_part<F32, AXES>(a, m, angles, t0, n, lane, Hk, a.k, a.k_stride, a.K, a.kv_row, a.kv_head, a.kw, a.kb, k);
+  if (norm) {
+    s_vec[threadIdx.x] = vec;
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (the rows stay on their way)
+  }
+  if (n <= 0) return;
+  ang.fill(a, t0, n, lane, angles);
+  prepare_part<F32, AXES, ONE>(a, pq, angles, lane, a.q, a.q_stride, a.Q, (int64_t)pq.H * D, D, s_vec, q);
+  prepare_part<F32, AXES, ONE>(a, pk, angles, lane, a.k, a.k_stride, a.K, a.kv_row, a.kv_head, s_vec + 2 * D, k);
+  if (!a.V) return;
+  for (int i = r; i < pk.count(); i += R) {
+    float x[E];
+    v.next(a.v, pk, i, a.v_stride, D, c, x);
+    store8<false, F32>(a.V, pk.at(i, a.kv_row, a.kv_head), c, x);
+  }
 }
 
 // Gradients.  dy is the incoming gradient turned back; with n the normed input, dw = sum dy n,
 // db = sum dy, and dx = r (e - [layer] mean(e) - n mean(e n)), e = dy w.  A lane adds up dw and db of
-// its 16 columns over its rows.
+// its 8 columns over its rows.
 struct Sums {
-  Pair16 dw, db;
+  float dw[E], db[E];
 };
 
-template <bool F32, int AXES>
-__device__ __forceinline__ void backward_part(const PrepArgs& a, const LaneMap<AXES>& m, const float2* angles, int t0, int n,
-                                              int lane, int H, const void* src, int64_t stride, const uint16_t* grad,
-                                              void* dst, int64_t dst_stride, const Pair16& w, Raw16<F32> raw,
-                                              Raw16<false> graw, Sums& sum) {
-  for (int r = lane >> 2; r < n * H; r += 16) {
-    const int t = n == 1 ? 0 : r / H, h = r - t * H;
-    Pair16 g, x;
-    unpack(graw, g);
-    unpack(raw, x);
-    if (r + 16 < n * H) {
-      const int t2 = n == 1 ? 0 : (r + 16) / H, h2 = r + 16 - t2 * H;
-      graw = load_raw<false>(grad, ((int64_t)(t0 + t2) * H + h2) * D, m.a, m.b);
-      if (a.norm != RV_NORM_NONE) raw = load_raw<F32>(src, (int64_t)(t0 + t2) * stride + h2 * D, m.a, m.b);
-    }
-    rotate<AXES, true>(angles + t * kAngles + m.angle, g);
+template <bool F32, int AXES, bool ONE>
+__device__ __forceinline__ void backward_part(const PrepArgs& a, const Rows<ONE>& p, const float2* angles, int lane, const void* src,
+                                              int64_t stride, const uint16_t* grad, void* dst, int64_t dst_stride,
+                                              const float* vecs, Ahead<F32, F32, ONE>& ahead, Ahead<false, F32, ONE>& grads, Sums& sum) {
+  const Cols<F32> c = lane_cols<F32, AXES>(lane);
+  for (int r = lane / 8; r < p.count(); r += R) {
+    float g[E];
+    grads.next(grad, p, r, (int64_t)p.H * D, D, c, g);
+    rotate<F32, AXES, true>(angles + p.token(r) * D, c, g);
     if (a.norm != RV_NORM_NONE) {
+      float x[E], w[E];
+      ahead.next(src, p, r, stride, D, c, x);
+      read_vec(vecs, c, w);
       const float rs = normalise(a.norm, a.eps, x);
       float se = 0.f, sn = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        sum.dw.a[i] = fmaf(g.a[i], x.a[i], sum.dw.a[i]);
-        sum.dw.b[i] = fmaf(g.b[i], x.b[i], sum.dw.b[i]);
-        sum.db.a[i] += g.a[i];
-        sum.db.b[i] += g.b[i];
-        g.a[i] *= w.a[i];
-        g.b[i] *= w.b[i];
-        se += g.a[i] + g.b[i];
-        sn = fmaf(g.a[i], x.a[i], fmaf(g.b[i], x.b[i], sn));
+      for (int i = 0; i < E; ++i) {
+        sum.dw[i] = fmaf(g[i], x[i], sum.dw[i]);
+        sum.db[i] += g[i];
+        g[i] *= w[i];
+        se += g[i];
+        sn = fmaf(g[i], x[i], sn);
       }
-      const float mn = head_sum(sn) * (1.f / D);
-      const float me = a.norm == RV_NORM_LAYER ? head_sum(se) * (1.f / D) : 0.f;
+      const float mn = row_sum(sn) * (1.f / D);
+      const float me = a.norm == RV_NORM_LAYER ? row_sum(se) * (1.f / D) : 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        g.a[i] = rs * (g.a[i] - me - x.a[i] * mn);
-        g.b[i] = rs * (g.b[i] - me - x.b[i] * mn);
-      }
+      for (int i = 0; i < E; ++i) g[i] = rs * (g[i] - me - x[i] * mn);
     }
-    const int64_t to = (int64_t)(t0 + t) * dst_stride + h * D;
-    store8<F32>(dst, to + m.a, g.a);
-    store8<F32>(dst, to + m.b, g.b);
+    store8<F32, F32>(dst, p.at(r, dst_stride, D), c, g);
   }
 }
 
-// Sum over the wave's 16 rows of head elements (lanes that differ in bits 2 to 5), of two values at a
-// time: lanes of the upper half go on with the second value, so that 64 sums take 60 exchanges rather than 256.
+// Sums over the wave's 8 rows of head elements (lanes that differ in bits 3 to 5), of two values at a
+// time: lanes of the upper half go on with the second value, so that 32 sums take 28 exchanges rather than 96.
 __device__ __forceinline__ float fold32(float x, float y) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
@@ -297,97 +353,66 @@ __device__ __forceinline__ float fold16(float x, float y) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-template <int CTRL>
-__device__ __forceinline__ float from_lane(float x) {
-  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true));
-}
-__device__ __forceinline__ float fold8(float x, float y, bool upper) {  // row_ror:8 is the lane 8 away
+__device__ __forceinline__ float fold8(float x, float y, bool upper) {
   const float keep = upper ? y : x, give = upper ? x : y;
-  return keep + from_lane<0x128>(give);
-}
-__device__ __forceinline__ float fold4(float x, float y, bool upper) {  // half-row mirror, quad reversed: 4 away
-  const float keep = upper ? y : x, give = upper ? x : y;
-  return keep + from_lane<0x1B>(from_lane<0x141>(give));
+  return keep + from_lane<kRotate8>(give);
 }
 
 // The block's sums go to part[block][q dw, q db, k dw, k db][64].
-template <bool F32, int AXES>
+template <bool F32, int AXES, bool ONE>
 __global__ __launch_bounds__(NT) void prepare_bwd_kernel(PrepArgs a) {
-  __shared__ float2 s_angles[NW][kPrepMaxTokens * kAngles];
+  __shared__ __attribute__((aligned(16))) float2 s_angles[NW][kPrepMaxTokens * D];
   __shared__ float s_sum[NW][4 * D];
+  __shared__ __attribute__((aligned(16))) float s_vec[4 * D];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Cols<F32> c = lane_cols<F32, AXES>(lane);
+  const int r = lane / 8;
   float2* const angles = s_angles[wave];
-  const LaneMap<AXES> m(lane & 3);
-  Sums sums[2] = {};
-  Pair16 w[2];
+  Sums sq = {}, sk = {};
   if (a.norm != RV_NORM_NONE) {
-    load_vec(a.qw, kOnes, m.a, m.b, w[0]);
-    load_vec(a.kw, kOnes, m.a, m.b, w[1]);
+    s_vec[threadIdx.x] = own_weight(a);
+    __syncthreads();
   }
-  const int Hq = a.n_q_heads, Hk = a.n_kv_heads, r = lane >> 2;
   const int64_t step = (int64_t)gridDim.x * NW * a.tokens_per_wave;
   for (int64_t first = ((int64_t)blockIdx.x * NW + wave) * a.tokens_per_wave; first < a.n_tokens; first += step) {
     const int t0 = (int)first, n = (int)min((int64_t)a.tokens_per_wave, a.n_tokens - first);
-    // The first rows of all parts are requested at once, before anything waits.
-    const int tq = n == 1 ? 0 : r / Hq, tk = n == 1 ? 0 : r / Hk;
-    const int hq = r - tq * Hq, hk = r - tk * Hk;
-    Raw16<F32> q{}, k{};
-    Raw16<false> gq{}, gk{}, gv{};
-    if (r < n * Hq) {
-      gq = load_raw<false>(a.dQ, ((int64_t)(t0 + tq) * Hq + hq) * D, m.a, m.b);
-      if (a.norm != RV_NORM_NONE) q = load_raw<F32>(a.q, (int64_t)(t0 + tq) * a.q_stride + hq * D, m.a, m.b);
+    const Rows<ONE> pq{t0, n, a.n_q_heads}, pk{t0, n, a.n_kv_heads};
+    Angles<AXES> ang;
+    Ahead<F32, F32, ONE> q, k;
+    Ahead<false, F32, ONE> gq, gk, gv;
+    ang.start(a, t0, n, lane);
+    gq.start(a.dQ, pq, r, (int64_t)pq.H * D, D, c);
+    gk.start(a.dK, pk, r, (int64_t)pk.H * D, D, c);
+    if (a.norm != RV_NORM_NONE) {
+      q.start(a.q, pq, r, a.q_stride, D, c);
+      k.start(a.k, pk, r, a.k_stride, D, c);
     }
-    if (r < n * Hk) {
-      gk = load_raw<false>(a.dK, ((int64_t)(t0 + tk) * Hk + hk) * D, m.a, m.b);
-      if (a.norm != RV_NORM_NONE) k = load_raw<F32>(a.k, (int64_t)(t0 + tk) * a.k_stride + hk * D, m.a, m.b);
-      if (a.dv) gv = load_raw<false>(a.dV, ((int64_t)(t0 + tk) * Hk + hk) * D, m.a, m.b);
-    }
-    if (AXES > 0) {
-      __builtin_amdgcn_wave_barrier();  // (the last tokens' angles have been read)
-      fill_angles<AXES>(a, t0, n, lane, angles);
-    }
-    backward_part<F32, AXES>(a, m, angles, t0, n, lane, Hq, a.q, a.q_stride, a.dQ, a.dq, a.dq_stride, w[0], q, gq, sums[0]);
-    backward_part<F32, AXES>(a, m, angles, t0, n, lane, Hk, a.k, a.k_stride, a.dK, a.dk, a.dk_stride, w[1], k, gk, sums[1]);
+    if (a.dv) gv.start(a.dV, pk, r, (int64_t)pk.H * D, D, c);
+    __builtin_amdgcn_wave_barrier();  // (the last tokens' angles have been read)
+    ang.fill(a, t0, n, lane, angles);
+    backward_part<F32, AXES, ONE>(a, pq, angles, lane, a.q, a.q_stride, a.dQ, a.dq, a.dq_stride, s_vec, q, gq, sq);
+    backward_part<F32, AXES, ONE>(a, pk, angles, lane, a.k, a.k_stride, a.dK, a.dk, a.dk_stride, s_vec + 2 * D, k, gk, sk);
     if (a.dv) {
-      for (int i = r; i < n * Hk; i += 16) {
-        const int t = n == 1 ? 0 : i / Hk, h = i - t * Hk;
-        Pair16 x;
-        unpack(gv, x);
-        if (i + 16 < n * Hk) {
-          const int t2 = n == 1 ? 0 : (i + 16) / Hk, h2 = i + 16 - t2 * Hk;
-          gv = load_raw<false>(a.dV, ((int64_t)(t0 + t2) * Hk + h2) * D, m.a, m.b);
-        }
-        const int64_t to = (int64_t)(t0 + t) * a.dv_stride + h * D;
-        store8<F32>(a.dv, to + m.a, x.a);
-        store8<F32>(a.dv, to + m.b, x.b);
+      for (int i = r; i < pk.count(); i += R) {
+        float x[E];
+        gv.next(a.dV, pk, i, (int64_t)pk.H * D, D, c, x);
+        store8<F32, F32>(a.dv, pk.at(i, a.dv_stride, D), c, x);
       }
     }
   }
   if (!a.part) return;
-  // Over the wave's 16 rows.  v[i], i = 8 c + e: element e of the lane's a (even c) or b (odd c) of q dw, q db,
-  // k dw, k db (c / 2).
-  float v[64];
+  // Over the wave's rows, then over the waves.
+  float v[32];
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
+  for (int i = 0; i < E; ++i) v[i] = sq.dw[i], v[8 + i] = sq.db[i], v[16 + i] = sk.dw[i], v[24 + i] = sk.db[i];
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      v[32 * p + e] = sums[p].dw.a[e];
-      v[32 * p + 8 + e] = sums[p].dw.b[e];
-      v[32 * p + 16 + e] = sums[p].db.a[e];
-      v[32 * p + 24 + e] = sums[p].db.b[e];
-    }
+  for (int i = 0; i < 16; ++i) v[i] = fold32(v[i], v[i + 16]);  // lanes 32 ..: the keys'
 #pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = fold32(v[i], v[i + 32]);  // lanes 32 ..: k's
+  for (int i = 0; i < 8; ++i) v[i] = fold16(v[i], v[i + 8]);  // lanes 16 .. of each half: db
 #pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = fold16(v[i], v[i + 16]);  // lanes 16 .. of each half: db
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = fold8(v[i], v[i + 8], lane & 8);  // lanes 8 .. of each row: b
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = fold4(v[i], v[i + 4], lane & 4);  // lanes 4 .. of each half row: elements 4 ..
-  {
-    const int col = (lane & 8 ? m.b : m.a) + (lane & 4), vec = 2 * (lane >> 5) + (lane >> 4 & 1);
-    *reinterpret_cast<float4*>(&s_sum[wave][vec * D + col]) = make_float4(v[0], v[1], v[2], v[3]);
-  }
+  for (int i = 0; i < 4; ++i) v[i] = fold8(v[i], v[i + 4], lane & 8);  // lanes 8 .. of each 16: elements 4 ..
+  const int vec = 2 * (lane >> 5) + (lane >> 4 & 1), col = (lane & 8) ? c.b : c.a;
+  *reinterpret_cast<float4*>(&s_sum[wave][vec * D + col]) = make_float4(v[0], v[1], v[2], v[3]);
   __syncthreads();
   for (int i = threadIdx.x; i < 4 * D; i += NT) {
     float t = 0.f;
@@ -417,26 +442,28 @@ __global__ __launch_bounds__(kSumCols* kSumGroups) void prepare_sum_kernel(const
   if (o) o[col % D] = t;
 }
 
-template <bool F32>
+template <bool F32, bool ONE>
 hipError_t launch(const PrepArgs& a, int axes, bool back, hipStream_t s) {
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)a.blocks), dim3(NT), 0, s, a);
     return hipGetLastError();
   };
   if (back)
-    return axes == 2   ? go(prepare_bwd_kernel<F32, 2>)
-           : axes == 1 ? go(prepare_bwd_kernel<F32, 1>)
-                       : go(prepare_bwd_kernel<F32, 0>);
-  return axes == 2   ? go(prepare_kernel<F32, 2>)
-         : axes == 1 ? go(prepare_kernel<F32, 1>)
-                     : go(prepare_kernel<F32, 0>);
+    return axes == 2   ? go(prepare_bwd_kernel<F32, 2, ONE>)
+           : axes == 1 ? go(prepare_bwd_kernel<F32, 1, ONE>)
+                       : go(prepare_bwd_kernel<F32, 0, ONE>);
+  return axes == 2   ? go(prepare_kernel<F32, 2, ONE>)
+         : axes == 1 ? go(prepare_kernel<F32, 1, ONE>)
+                     : go(prepare_kernel<F32, 0, ONE>);
 }
 
 }  // namespace
 
 hipError_t launch_prepare(const PrepArgs& a, bool f32, int axes, bool back, hipStream_t s) {
   if (a.n_tokens > 0) {
-    const hipError_t e = f32 ? launch<true>(a, axes, back, s) : launch<false>(a, axes, back, s);
+    const bool one = a.tokens_per_wave == 1;
+    const hipError_t e = f32 ? (one ? launch<true, true>(a, axes, back, s) : launch<true, false>(a, axes, back, s))
+                             : (one ? launch<false, true>(a, axes, back, s) : launch<false, false>(a, axes, back, s));
     if (e != hipSuccess) return e;
   }
   if (!a.dqw && !a.dqb && !a.dkw && !a.dkb) return hipSuccess;

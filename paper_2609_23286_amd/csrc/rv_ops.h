@@ -19,7 +19,8 @@ constexpr int kMaxGridBlocks = 1 << 23;
 
 constexpr int kMaxFreqs = kHeadDim / 2;
 constexpr int kPrepThreads = 256;
-constexpr int kPrepMaxTokens = 16;  // tokens a wave takes at a time
+constexpr int kPrepRows = 8;       // heads a wave takes at a time
+constexpr int kPrepMaxTokens = 8;  // tokens a wave takes at a time
 
 // Source and gradient rows are [n_tokens] rows of `stride` elements, head h at column 64 h.
 struct PrepArgs {

@@ -58,11 +58,11 @@ rv::PrepArgs base_args(const rv_qkv_prep& p, int n_tokens, const int32_t* pos) {
   return a;
 }
 
-// As many tokens a wave as fill its 16 rows of heads: more rows in a wave were slower than more waves
+// As many tokens a wave as fill its rows of heads: more rows in a wave were slower than more waves
 // (8328 tokens of 16 heads: 27 us at three tokens a wave, 20 at one).
 void plan_waves(rv::PrepArgs* a, int max_blocks) {
   const int heads = std::max(a->n_q_heads, a->n_kv_heads);
-  a->tokens_per_wave = std::min(rv::kPrepMaxTokens, std::max(1, 16 / heads));
+  a->tokens_per_wave = std::min(rv::kPrepMaxTokens, std::max(1, rv::kPrepRows / heads));
   const int64_t blocks = rv::ceil_div64(a->n_tokens, (int64_t)a->tokens_per_wave * (rv::kPrepThreads / 64));
   a->blocks = (int)std::min<int64_t>(blocks, max_blocks);
 }
