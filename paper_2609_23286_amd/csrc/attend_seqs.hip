@@ -91,22 +91,162 @@ struct TileOrder {
   }
 };
 
-// A tile's K and V into a ring stage by the whole workgroup, 16 bytes a thread and row pair.
-__device__ __forceinline__ void load_tile(const TileRows& ts, uint16_t* st) {
-  const uint32_t r = threadIdx.x >> 3, c = threadIdx.x & 7;
-  const uint32_t o0 = min(r, ts.last) * ts.row + 16u * (c ^ sw(r));
-  const uint32_t o1 = min(r + 32, ts.last) * ts.row + 16u * (c ^ sw(r + 32));
-  lds_load16(ts.k + o0, st);
-  lds_load16(ts.k + o1, st + 32 * D);
-  lds_load16(ts.v + o0, st + TILE);
-  lds_load16(ts.v + o1, st + TILE + 32 * D);
-}
-
 // Lane l's 16 bytes at base + off go to LDS byte lds + 16 l.  (Assembly: the compiler would wait for
 // every such load in flight before each LDS read.  No register is written.  The wait states are
 // those a scalar that a vector instruction wrote needs before a load reads it.)
 __device__ __forceinline__ void lds_load16_asm(const char* base, uint32_t off, uint32_t lds) {
   asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
+}
+
+// A tile's K and V into a ring stage by the whole workgroup: `st` is the LDS byte of the stage plus
+// this wave's row block (rows 8w .. 8w + 7; the second load of each fills rows 32 + 8w ..).
+__device__ __forceinline__ void load_tile(const TileRows& ts, uint32_t st) {
+  const uint32_t r = threadIdx.x >> 3, c = threadIdx.x & 7;
+  const uint32_t o0 = min(r, ts.last) * ts.row + 16u * (c ^ sw(r));
+  const uint32_t o1 = min(r + 32, ts.last) * ts.row + 16u * (c ^ sw(r + 32));
+  lds_load16_asm(ts.k, o0, st);
+  lds_load16_asm(ts.k, o1, st + 32 * D * 2);
+  lds_load16_asm(ts.v, o0, st + TILE * 2);
+  lds_load16_asm(ts.v, o1, st + TILE * 2 + 32 * D * 2);
+}
+
+// ---- 32 queries over NB blocks of 32 keys -----------------------------------------------------
+
+// Scores: entry r of s[i] is key 32 i + 8 (r / 4) + 4 half + r % 4.
+template <int NB>
+struct Scores {
+  f32x16 s[NB];
+};
+template <int NB>
+__device__ __forceinline__ void read_keys(const uint16_t* keys, int lane, bf16x8 (&kf)[NB][4]) {
+#pragma unroll
+  for (int ds = 0; ds < 4; ++ds)
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+      kf[i][ds] = *reinterpret_cast<const bf16x8*>(&keys[swz(32 * i + (lane & 31), ds * 2 + (lane >> 5))]);
+}
+template <int NB>
+__device__ __forceinline__ void score(const bf16x8 (&kf)[NB][4], const bf16x8 (&qf)[4], Scores<NB>& z) {
+#pragma unroll
+  for (int i = 0; i < NB; ++i) z.s[i] = f32x16{};
+#pragma unroll
+  for (int ds = 0; ds < 4; ++ds)
+#pragma unroll
+    for (int i = 0; i < NB; ++i) z.s[i] = mfma32(kf[i][ds], qf[ds], z.s[i]);
+}
+// Keys >= valid get -1e30 (arithmetically: lane masks would take the scalar registers).
+template <int NB>
+__device__ __forceinline__ void mask_scores(Scores<NB>& z, int lane, int valid) {
+  const float fv = (float)(valid - 4 * (lane >> 5) - 1);
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      z.s[i][r] = fmaf(__saturatef((float)(32 * i + 8 * (r >> 2) + (r & 3)) - fv), kNegBig, z.s[i][r]);
+}
+// p = 2^(z log2(e) / 8 - m), rounded to bf16 as the value product's operand; returns this lane's share of their
+// sum, of the unrounded ones (summed after rounding, two to an instruction, the log-sum-exp of 63 keys was 2e-4 off).
+template <int NB>
+__device__ __forceinline__ float exponentials(const Scores<NB>& z, float m, bf16x8 (&p)[2 * NB]) {
+  float sum = -0.f;  // -0 + x == x: the first add folds away
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(z.s[i][r], kScaleLog2, -m));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(z.s[i][r + 1], kScaleLog2, -m));
+      sum += e0 + e1;
+      p[2 * i + (r >> 3)][r & 7] = (__bf16)e0;
+      p[2 * i + (r >> 3)][(r & 7) + 1] = (__bf16)e1;
+    }
+  return sum;
+}
+// The end of the keys' softmax, by tile_compute's rule: where some lane's sum reaches 2^64 (every p is infinite while
+// the reference is unset), the reference is raised to the keys' maximum and p formed again.
+template <int NB>
+__device__ __forceinline__ void settle(const Scores<NB>& z, SoftmaxState& sm, bf16x8 (&p)[2 * NB], float sum) {
+  if (__builtin_expect(__any(!(sum < kOverflowGuard)), 0)) {
+    float mx = z.s[0][0];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, z.s[i][r]);
+    const float m_new = fmaxf(sm.m, half_max(mx) * kScaleLog2);
+    const float alpha = __builtin_amdgcn_exp2f(sm.m - m_new);
+    sm.l *= alpha;
+    sm.o0 *= alpha;
+    sm.o1 *= alpha;
+    sm.m = m_new;
+    sum = exponentials(z, m_new, p);
+  }
+  sm.l += sum;
+}
+// V^T fragments through transposing reads, as in tile_compute.
+template <int NB>
+__device__ __forceinline__ void read_values(const uint16_t* values, int lane, bf16x8 (&vf)[2 * NB][2]) {
+  const int g = lane >> 4, i16 = lane & 15, rr = i16 >> 2, jj = i16 & 3, hh = g >> 1;
+  const int col = 16 * (g & 1) + 4 * jj;
+#pragma unroll
+  for (int ks = 0; ks < 2 * NB; ++ks)
+#pragma unroll
+    for (int db = 0; db < 2; ++db) {
+      const int row = ks * 16 + 4 * hh + rr, lcol = db * 32 + col;
+      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(values + swz(row, lcol >> 3) + (lcol & 7)));
+      const i16x4 hi =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(values + swz(row + 8, lcol >> 3) + (lcol & 7)));
+      vf[ks][db] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+}
+template <int NB>
+__device__ __forceinline__ void add_values(const bf16x8 (&vf)[2 * NB][2], const bf16x8 (&p)[2 * NB], SoftmaxState& sm) {
+#pragma unroll
+  for (int ks = 0; ks < 2 * NB; ++ks) {
+    sm.o0 = mfma32(vf[ks][0], p[ks], sm.o0);
+    sm.o1 = mfma32(vf[ks][1], p[ks], sm.o1);
+  }
+}
+
+// Keys and values in LDS, all of them at once.
+template <int NB>
+__device__ __forceinline__ void compute(const uint16_t* keys, const uint16_t* values, const bf16x8 (&qf)[4], int lane,
+                                        int valid, SoftmaxState& sm) {
+  Scores<NB> z;
+  bf16x8 kf[NB][4], vf[2 * NB][2], p[2 * NB];
+  read_keys<NB>(keys, lane, kf);
+  score(kf, qf, z);
+  if (__builtin_expect(valid < 32 * NB, 0)) mask_scores(z, lane, valid);
+  read_values<NB>(values, lane, vf);
+  settle(z, sm, p, exponentials(z, sm.m, p));
+  add_values<NB>(vf, p, sm);
+}
+
+// Two tiles: the scores of b are formed under the exponentials of a, and the value product of a under the
+// exponentials of b.  (Against one tile after the other: 4 to 5 % less where keys come from memory, 240 queries over
+// 52,000 rows, and the same within 1 % where they are in L2: there the two waves of a SIMD share its units to
+// the same effect whatever the order within a wave.)
+__device__ __forceinline__ void compute_pair(const uint16_t* a, const uint16_t* b, const bf16x8 (&qf)[4], int lane,
+                                             int valid_a, int valid_b, SoftmaxState& sm) {
+  Scores<2> za, zb;
+  bf16x8 kf[2][4], vf[4][2], pa[4], pb[4];
+  read_keys<2>(a, lane, kf);
+  score(kf, qf, za);
+  if (__builtin_expect(valid_a < BK, 0)) mask_scores(za, lane, valid_a);
+  __builtin_amdgcn_sched_barrier(0);
+  read_keys<2>(b, lane, kf);
+  read_values<2>(a + TILE, lane, vf);
+  __builtin_amdgcn_sched_barrier(0);
+  score(kf, qf, zb);
+  const float sum_a = exponentials(za, sm.m, pa);
+  __builtin_amdgcn_sched_barrier(0);
+  settle(za, sm, pa, sum_a);
+  if (__builtin_expect(valid_b < BK, 0)) mask_scores(zb, lane, valid_b);
+  __builtin_amdgcn_sched_barrier(0);
+  add_values<2>(vf, pa, sm);
+  const float sum_b = exponentials(zb, sm.m, pb);
+  __builtin_amdgcn_sched_barrier(0);
+  read_values<2>(b + TILE, lane, vf);
+  settle(zb, sm, pb, sum_b);
+  add_values<2>(vf, pb, sm);
 }
 
 // ---- few queries: every wave takes tiles of its own -------------------------------------------
@@ -134,80 +274,6 @@ __device__ __forceinline__ void load_half(const TileRows& ts, int hk, uint32_t s
       const uint32_t off = min(r + kHalf * hk, ts.last) * ts.row + 16u * (c ^ sw(r));
       lds_load16_asm(ts.k, off, st + i * 8 * D * 2);
       lds_load16_asm(ts.v, off, st + kHalf * D * 2 + i * 8 * D * 2);
-    }
-  }
-}
-
-// 32 keys for the wave's NQ blocks of 32 queries; tile_compute's arithmetic.  Each fragment read from LDS
-// serves all blocks.  (Before the first keys the reference is kNegBig: every p is then infinite and
-// the exact path sets it.)
-template <int NQ>
-__device__ __forceinline__ void half_compute(const uint16_t* stage, const bf16x8 (&qf)[NQ][4], int lane, int valid,
-                                             SoftmaxState (&sm)[NQ]) {
-  const int l32 = lane & 31, half = lane >> 5;
-  bf16x8 kf[4];
-#pragma unroll
-  for (int ds = 0; ds < 4; ++ds) kf[ds] = *reinterpret_cast<const bf16x8*>(&stage[swz(l32, ds * 2 + half)]);
-  bf16x8 p[NQ][2];
-#pragma unroll
-  for (int b = 0; b < NQ; ++b) {
-    f32x16 s = {};
-#pragma unroll
-    for (int ds = 0; ds < 4; ++ds) s = mfma32(kf[ds], qf[b][ds], s);
-    if (valid < kHalf) {
-      const float fv = (float)(valid - 4 * half - 1);
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        s[r] = fmaf(__saturatef((float)(8 * (r >> 2) + (r & 3)) - fv), kNegBig, s[r]);
-    }
-    float rsum;
-    auto exponentials = [&]() {
-      rsum = -0.f;
-#pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[r], kScaleLog2, -sm[b].m));
-        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[r + 1], kScaleLog2, -sm[b].m));
-        rsum += e0 + e1;
-        p[b][r >> 3][r & 7] = (__bf16)e0;
-        p[b][r >> 3][(r & 7) + 1] = (__bf16)e1;
-      }
-    };
-    exponentials();
-    if (__any(!(rsum < kOverflowGuard))) {
-      float mx = s[0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-      const float m_new = fmaxf(sm[b].m, half_max(mx) * kScaleLog2);
-      const float alpha = __builtin_amdgcn_exp2f(sm[b].m - m_new);
-      sm[b].l *= alpha;
-      sm[b].o0 *= alpha;
-      sm[b].o1 *= alpha;
-      sm[b].m = m_new;
-      exponentials();
-    }
-    sm[b].l += rsum;
-    if (NQ > 1) __builtin_amdgcn_sched_barrier(0);  // (one block's scores at a time: registers)
-  }
-  // V^T through transposing reads, as in tile_compute
-  const uint16_t* vt = stage + kHalf * D;
-  const int g = lane >> 4, i16 = lane & 15, rr = i16 >> 2, jj = i16 & 3, hh = g >> 1;
-  const int col = 16 * (g & 1) + 4 * jj;
-#pragma unroll
-  for (int ks = 0; ks < 2; ++ks) {
-    const int row = ks * 16 + 4 * hh + rr;
-#pragma unroll
-    for (int db = 0; db < 2; ++db) {
-      const int lcol = db * 32 + col;
-      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vt + swz(row, lcol >> 3) + (lcol & 7)));
-      const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vt + swz(row + 8, lcol >> 3) + (lcol & 7)));
-      const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-      for (int b = 0; b < NQ; ++b) {
-        if (db == 0)
-          sm[b].o0 = mfma32(va, p[b][ks], sm[b].o0);
-        else
-          sm[b].o1 = mfma32(va, p[b][ks], sm[b].o1);
-      }
     }
   }
 }
@@ -267,23 +333,20 @@ __device__ __forceinline__ void load_queries(const SeqArgs& a, const SeqPass& p,
 
 // Few queries: the waves share them and take every fourth tile each, half a tile at a time through
 // two stages of their own, without barriers; the loads of the next half run under this one's work.
-template <int NQ>
 __device__ __forceinline__ void narrow_segment(const SeqArgs& a, const SeqPass& p, const SeqCursor& tc, const Segment& g,
                                                uint16_t* lds, float (*s_m)[kSubRows], float (*s_l)[kSubRows]) {
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
-  const int q0 = g.qt * NQ * kSubRows;
-  bf16x8 qf[NQ][4];
-  SoftmaxState sm[NQ];
-#pragma unroll
-  for (int b = 0; b < NQ; ++b) {
-    load_queries(a, p, g.h, q0 + b * kSubRows, lane, qf[b]);
-    sm[b].m = kNegBig;
-    sm[b].l = 0.f;
-    sm[b].o0 = f32x16{};
-    sm[b].o1 = f32x16{};
-  }
+  const int q0 = g.qt * kSubRows;
+  bf16x8 qf[4];
+  load_queries(a, p, g.h, q0, lane, qf);
+  SoftmaxState sm;
+  sm.m = kNegBig;
+  sm.l = 0.f;
+  sm.o0 = f32x16{};
+  sm.o1 = f32x16{};
   const uint32_t ring = (uint32_t)(uintptr_t)(lds_void*)(lds + wave * 2 * kHalfStage);
-  const uint16_t* const stage = lds + wave * 2 * kHalfStage;
+  const uint16_t* const st0 = lds + wave * 2 * kHalfStage;
+  const uint16_t* const st1 = st0 + kHalfStage;
   const int n = g.t1 - g.t0 > wave ? (g.t1 - g.t0 - wave + 3) / 4 : 0;  // tiles of this wave
   TileOrder order{g.t0 + wave, 4};
   TileRows next{};
@@ -292,9 +355,7 @@ __device__ __forceinline__ void narrow_segment(const SeqArgs& a, const SeqPass& 
     next = order.rows(tc, 0);
   }
   // (the queries pass through a wait here: the compiler's own for them would wait for the tiles too)
-#pragma unroll
-  for (int b = 0; b < NQ; ++b)
-    asm volatile("s_waitcnt vmcnt(0)" : "+v"(qf[b][0]), "+v"(qf[b][1]), "+v"(qf[b][2]), "+v"(qf[b][3])::"memory");
+  asm volatile("s_waitcnt vmcnt(0)" : "+v"(qf[0]), "+v"(qf[1]), "+v"(qf[2]), "+v"(qf[3])::"memory");
   if (n > 0) {
     load_half(next, 0, ring, lane);
     load_half(next, 1, ring + kHalfStage * 2, lane);
@@ -304,7 +365,7 @@ __device__ __forceinline__ void narrow_segment(const SeqArgs& a, const SeqPass& 
     const bool more = i + 1 < n;
     if (more) next = order.rows(tc, i + 1);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kHalfLoads) : "memory");
-    half_compute<NQ>(stage, qf, lane, valid, sm);
+    compute<1>(st0, st0 + kHalf * D, qf, lane, valid, sm);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) {
       load_half(next, 0, ring, lane);
@@ -312,43 +373,40 @@ __device__ __forceinline__ void narrow_segment(const SeqArgs& a, const SeqPass& 
     } else {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
-    if (valid > kHalf) half_compute<NQ>(stage + kHalfStage, qf, lane, valid - kHalf, sm);
+    if (valid > kHalf) compute<1>(st1, st1 + kHalf * D, qf, lane, valid - kHalf, sm);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) load_half(next, 1, ring + kHalfStage * 2, lane);
   }
-  // The four waves' sums meet in LDS, a block of queries at a time.
+  // The four waves' sums meet in LDS.
+  const float l_tot = half_sum(sm.l);
+  __syncthreads();
   float* const st = reinterpret_cast<float*>(lds);
+  stage_rows(sm, st + wave * kSubRows * kRowStride, lane);
+  if (half == 0) {
+    s_m[wave][l32] = sm.m;
+    s_l[wave][l32] = l_tot;
+  }
+  __syncthreads();
+  const int rr = tid >> 3, d8 = (tid & 7) * 8, r = q0 + rr;
+  if (r < p.n_tok * a.group) {
+    float m = s_m[0][rr];
 #pragma unroll
-  for (int b = 0; b < NQ; ++b) {
-    const float l_tot = half_sum(sm[b].l);
-    __syncthreads();
-    stage_rows(sm[b], st + wave * kSubRows * kRowStride, lane);
-    if (half == 0) {
-      s_m[wave][l32] = sm[b].m;
-      s_l[wave][l32] = l_tot;
+    for (int w = 1; w < 4; ++w) m = fmaxf(m, s_m[w][rr]);
+    float l = 0.f, o[8] = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = __builtin_amdgcn_exp2f(s_m[w][rr] - m);
+      l = fmaf(f, s_l[w][rr], l);
+      const float* x = st + (w * kSubRows + rr) * kRowStride + d8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = fmaf(f, x[e], o[e]);
     }
-    __syncthreads();
-    const int rr = tid >> 3, d8 = (tid & 7) * 8, r = q0 + b * kSubRows + rr;
-    if (r < p.n_tok * a.group) {
-      float m = s_m[0][rr];
-#pragma unroll
-      for (int w = 1; w < 4; ++w) m = fmaxf(m, s_m[w][rr]);
-      float l = 0.f, o[8] = {};
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float f = __builtin_amdgcn_exp2f(s_m[w][rr] - m);
-        l = fmaf(f, s_l[w][rr], l);
-        const float* x = st + (w * kSubRows + rr) * kRowStride + d8;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = fmaf(f, x[e], o[e]);
-      }
-      write_row(a, p, g.h, r, d8, o, m, l, g.slots ? g.slots + b * kSubFloats : nullptr);
-    }
+    write_row(a, p, g.h, r, d8, o, m, l, g.slots);
   }
   __syncthreads();  // (the LDS is the next segment's)
 }
 
-// The ring of attend.hip: two tiles computed per barrier while the next two stream in.
+// Many queries: 32 to a wave, and a ring of four tiles, two computed per barrier while the next two stream in.
 __device__ __forceinline__ void wide_segment(const SeqArgs& a, const SeqPass& p, const SeqCursor& tc, const Segment& g,
                                              uint16_t* lds, float (*s_m)[kSubRows], float (*s_l)[kSubRows]) {
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
@@ -361,29 +419,30 @@ __device__ __forceinline__ void wide_segment(const SeqArgs& a, const SeqPass& p,
   sm.o0 = f32x16{};
   sm.o1 = f32x16{};
   const bool active = q0 < rows;
-  uint16_t* const ldsw = lds + wave * 8 * D;
   TileOrder order{t0, 1};
   order.fetch(tc, 0);
-  auto step = [&](auto phase, auto first, int t) {
+  const uint32_t ring = (uint32_t)(uintptr_t)(lds_void*)lds + wave * 8 * D * 2;
+  constexpr uint32_t kStageBytes = STAGE * 2;
+  load_tile(order.rows(tc, 0), ring);
+  if (t0 + 1 < t1) load_tile(order.rows(tc, 1), ring + kStageBytes);
+  // (the queries pass through the wait: the compiler's own for them would wait for tiles in the loop)
+  asm volatile("s_waitcnt vmcnt(0)" : "+v"(qf[0]), "+v"(qf[1]), "+v"(qf[2]), "+v"(qf[3])::"memory");
+  __syncthreads();
+  auto step = [&](auto phase, int t) {
     constexpr int P = decltype(phase)::value;
-    if (t + 2 < t1) load_tile(order.rows(tc, t + 2 - t0), ldsw + (P + 2) % NSTAGE * STAGE);
-    if (t + 3 < t1) load_tile(order.rows(tc, t + 3 - t0), ldsw + (P + 3) % NSTAGE * STAGE);
-    if (active) {
-      tile_compute<decltype(first)::value>(lds + P * STAGE, qf, lane, tc.valid(t), sm);
-      if (t + 1 < t1) tile_compute<false>(lds + (P + 1) * STAGE, qf, lane, tc.valid(t + 1), sm);
-    }
+    if (t + 2 < t1) load_tile(order.rows(tc, t + 2 - t0), ring + (P + 2) % NSTAGE * kStageBytes);
+    if (t + 3 < t1) load_tile(order.rows(tc, t + 3 - t0), ring + (P + 3) % NSTAGE * kStageBytes);
+    if (active && t + 1 < t1)
+      compute_pair(lds + P * STAGE, lds + (P + 1) * STAGE, qf, lane, tc.valid(t), tc.valid(t + 1), sm);
+    else if (active)
+      compute<2>(lds + P * STAGE, lds + P * STAGE + TILE, qf, lane, tc.valid(t), sm);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
-  load_tile(order.rows(tc, 0), ldsw);
-  if (t0 + 1 < t1) load_tile(order.rows(tc, 1), ldsw + STAGE);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  step(StageConst<0>{}, std::true_type{}, t0);
-  for (int t = t0 + 2; t < t1; t = uniform(t + 4)) {
-    step(StageConst<2>{}, std::false_type{}, t);
+  for (int t = t0; t < t1; t = uniform(t + 4)) {
+    step(StageConst<0>{}, t);
     if (t + 2 >= t1) break;
-    step(StageConst<0>{}, std::false_type{}, t + 2);
+    step(StageConst<2>{}, t + 2);
   }
 
   // Rows through LDS, so that whole rows are written (the ring is free: the last step ended in a barrier).
@@ -455,7 +514,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
     tc.last_rows = p.last_rows;
     tc.frame_rows = p.frame > 0 ? p.frame - (T - p.n_pages - 1) * BK : p.last_rows;
     if (p.tile_rows == kSubRows)
-      narrow_segment<1>(a, p, tc, g, lds, s_m, s_l);
+      narrow_segment(a, p, tc, g, lds, s_m, s_l);
     else
       wide_segment(a, p, tc, g, lds, s_m, s_l);
     pos = g.t1 < T ? end : seq_pos(p, unit + 1, 0);
