@@ -384,9 +384,13 @@ rv_status rv_prepare_qkv_bwd(const rv_qkv_prep *p, const void *q, int64_t q_stri
  * of RV_PAGE_ROWS rows of every head, K and V [n_pages][n_heads][64][64] bf16.  A sequence is a
  * list of pages; forked sequences share pages, and a page returns to the pool when its last
  * user drops it.  Rows never move except in rv_pool_compact.  Lengths and lists are kept on the host
- * as enqueued (no device sync); the device's copy of the lists is written by kernels, in
- * stream order, so the calls can be captured: a captured call keeps the rows and pages it was
- * enqueued with.  Calls on one pool must be ordered on one stream.  On failure nothing changes. */
+ * as enqueued (no device sync); the device's copy of the lists is written by kernels, in stream order.
+ * Calls on one pool must be ordered on one stream, and so must the calls that name its sequences.  On
+ * failure nothing changes (RV_ERR_HIP from a launch excepted).  The calls allocate nothing and can be
+ * captured.  A captured call repeats what it was enqueued with, lengths, rows and pages; it stays valid
+ * while the sequences it names keep those pages (are not closed, compacted, or cut below those lengths)
+ * and no other call writes the same rows.  Values are taken to be finite; rows past a sequence's end may
+ * hold anything.  One call moves at most 2^28 rows x heads of one sequence. */
 #define RV_PAGE_ROWS 64
 typedef struct rv_pool_s *rv_pool;
 

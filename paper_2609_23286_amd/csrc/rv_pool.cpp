@@ -170,10 +170,7 @@ rv_status rv_pool_create(int n_heads, int head_dim, int n_pages, int max_seqs, i
   rv_status st = rv::setup_sequences();
   if (st != RV_OK) return st;
   rv_pool p = new (std::nothrow) rv_pool_s;
-  if (!p || !p->book.init(n_pages, max_seqs, (int)width)) {
-    delete p;
-    return fail(RV_ERR_OOM, "host allocation failed");
-  }
+  if (!p) return fail(RV_ERR_OOM, "host allocation failed");
   p->n_heads = n_heads;
   p->max_rows = max_rows;
   const size_t bytes = (size_t)n_pages * n_heads * kPageRows * rv::kHeadDim * 2;
@@ -185,6 +182,10 @@ rv_status rv_pool_create(int n_heads, int head_dim, int n_pages, int max_seqs, i
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e != hipSuccess) {
     st = rv::hip_fail(e, "page pool allocation");
+  } else if (!p->book.init(n_pages, max_seqs, (int)width)) {  // (after the device's: a size it has room for)
+    st = fail(RV_ERR_OOM, "host allocation failed");
+  }
+  if (st != RV_OK) {
     (void)hipGetLastError();
     (void)hipFree(p->K);
     (void)hipFree(p->V);

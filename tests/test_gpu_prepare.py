@@ -273,3 +273,47 @@ def test_captured_and_on_another_stream(rv):
         got = backward(rv, x)
         names = ("dq", "dk", "dv", "dq_weight", "dq_bias", "dk_weight", "dk_bias")
         assert all(torch.equal(got[n], t) for n, t in zip(names, grads + vecs))
+
+
+def test_rows_far_apart(rv):
+    """Element offsets past 2^31."""
+    N, stride = 9000, 300_000
+    wide = torch.empty(N * stride, dtype=torch.bfloat16, device="cuda").view(N, stride)
+    x = Case(rv, N, 2, 1, norm="rms")
+    q, k, v = wide[:, 128:256], wide[:, 512:576], wide[:, 299_904:299_968]
+    for far, near in ((q, x.q), (k, x.k), (v, x.v)):
+        far.copy_(near)
+    Q, K, V = (t[:N] for t in x.empty())
+    rv.prepare_qkv(x.prep, q, k, v, x.pos, Q, K, V)
+    near = [torch.empty_like(t) for t in (Q, K, V)]
+    rv.prepare_qkv(x.prep, x.q, x.k, x.v, x.pos, *near)
+    assert all(torch.equal(a, b) for a, b in zip((Q, K, V), near))
+    want = backward(rv, x)
+    sums = {n: torch.empty(D, device="cuda") for n in ("dq_weight", "dq_bias", "dk_weight", "dk_bias")}
+    grads = wide[:, 1024:1152], wide[:, 2048:2112], wide[:, 4096:4160]
+    rv.prepare_qkv_bwd(x.prep, q, k, x.pos, x.dQ, x.dK, x.dV, *grads, **sums)
+    assert all(torch.equal(a, want[n]) for a, n in zip(grads, ("dq", "dk", "dv")))
+    assert all(torch.equal(sums[n], want[n]) for n in sums)
+
+
+def test_the_binding_refuses_before_the_launch(rv):
+    x = Case(rv, 5, 2, 1)
+    Q, K, V = (t[:5] for t in x.empty())
+    for call, words in (
+            (lambda: rv.prepare_qkv(x.prep, x.q[:, :64], x.k, x.v, x.pos, Q, K, V), "q: shape"),
+            (lambda: rv.prepare_qkv(x.prep, x.q, x.k[:4], x.v, x.pos, Q, K, V), "4 rows, expected 5"),
+            (lambda: rv.prepare_qkv(x.prep, x.q, x.k.float(), x.v, x.pos, Q, K, V), "another dtype"),
+            (lambda: rv.prepare_qkv(x.prep, x.q.half(), x.k, x.v, x.pos, Q, K, V), "dtype"),
+            (lambda: rv.prepare_qkv(x.prep, x.q.t().contiguous().t(), x.k, x.v, x.pos, Q, K, V), "contiguous"),
+            (lambda: rv.prepare_qkv(x.prep, x.q, x.k, x.v, x.pos.long(), Q, K, V), "pos: dtype"),
+            (lambda: rv.prepare_qkv(x.prep, x.q, x.k, x.v, x.pos[:, :1], Q, K, V), "pos"),
+            (lambda: rv.prepare_qkv(x.prep, x.q, x.k, x.v, None, Q, K, V), "pos is required"),
+            (lambda: rv.prepare_qkv(x.prep, x.q, x.k, x.v, x.pos, Q[:, :1], K, V), "Q"),
+            (lambda: rv.prepare_qkv(x.prep, x.q, x.k, x.v, x.pos, Q, K, None), "both"),
+            (lambda: rv.prepare_qkv(x.prep, x.q.cpu(), x.k, x.v, x.pos, Q, K, V), "device tensor"),
+            (lambda: rv.prepare_qkv(x.prep, x.q[:1].expand(5, -1), x.k, x.v, x.pos, Q, K, V), "row stride"),
+            (lambda: backward(rv, Case(rv, 5, 2, 1, norm=None), True) and rv.prepare_qkv_bwd(
+                x.prep, x.q, x.k, x.pos, x.dQ, x.dK, x.dV, x.q.float(), x.k, x.v), "another dtype")):
+        with pytest.raises((rv.RVError, ValueError, TypeError), match=words):
+            call()
+    assert all(bool((t == 7).all()) for t in (Q, K, V))

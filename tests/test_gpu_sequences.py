@@ -456,3 +456,218 @@ def test_admission_of_more_sequences_than_a_launch_takes(rv):
     want = K.transpose(1, 2).gather(2, idx.long()[..., None].expand(-1, -1, -1, D))
     assert torch.equal(gk, want)
     assert torch.equal(sal.topk(k, dim=2).indices.sort(2).values.int(), idx)
+
+
+# ---- refusals, bindings, graphs, sizes -----------------------------------------------------------
+
+def refused(rv, status, words, call, *args, **kw):
+    with pytest.raises(rv.RVError, match=words) as e:
+        call(*args, **kw)
+    assert e.value.status == status
+
+
+def test_refusals_change_nothing(rv):
+    w = World(rv, 2, 10, 5, 300)  # 3 pages taken below; the appends refused for pages need 8, the compaction 10
+    pool = w.pool
+    a, b = w.open(), w.open()
+    w.append([a, b], [100, 64])
+    c = w.fork(a, 90)[0]
+    free = pool.free_pages
+    K = rand(w.g, 400, 2, D)
+    INV, CAP = rv.RV_ERR_INVALID, rv.RV_ERR_CAPACITY
+    gone = w.open()
+    w.release([gone])
+    refused(rv, INV, "named twice", pool.append, [a, a], K[:2], K[:2], [1, 1])
+    refused(rv, INV, "not open", pool.append, [gone], K[:1], K[:1], [1])
+    refused(rv, INV, "not open", pool.append, [-1], K[:1], K[:1], [1])
+    refused(rv, INV, "not open", pool.append, [5], K[:1], K[:1], [1])
+    refused(rv, CAP, "max_rows", pool.append, [a, b], K[:202], K[:202], [1, 201][::-1])
+    refused(rv, INV, "K and V are required", pool.append, [a], None, K[:1], [1])
+    refused(rv, CAP, "pages", pool.append, [a, b, c], K, K, [150, 100, 150])
+    with pytest.raises(ValueError, match="shape"):
+        pool.append([a], K[:2], K[:2], [1])
+    with pytest.raises(ValueError, match="contiguous"):
+        pool.append([a], K[:2, :, :].transpose(0, 1).contiguous().transpose(0, 1), K[:2], [2])
+    refused(rv, INV, "n_rows", pool.fork, a, 101)
+    refused(rv, INV, "n_rows", pool.fork, a, -1)
+    refused(rv, INV, "not open", pool.fork, gone, 0)
+    refused(rv, CAP, "can be opened", pool.fork, a, 10, 3)
+    refused(rv, INV, "n_rows", pool.truncate, a, 101)
+    refused(rv, INV, "named twice", pool.release, [b, b])
+    refused(rv, INV, "rows", pool.gather, [a], K[:2].view(4, D), None, [2], [99])
+    refused(rv, INV, "rows", pool.gather, [a], K[:2].view(4, D), None, [2], [-1])
+    keep = torch.zeros(2 * 500, dtype=torch.int32, device="cuda")
+    refused(rv, INV, "first", pool.compact, [a], keep[:2], [1], [101])
+    refused(rv, CAP, "max_rows", pool.compact, [a], keep[:2 * 250], [250], [64])
+    refused(rv, CAP, "pages", pool.compact, [a, b, c], keep, [200, 140, 160], [0, 0, 0])
+    refused(rv, INV, "keep is NULL", pool.compact, [a], None, [1], [0])
+    with pytest.raises(ValueError, match="keep"):
+        pool.compact([a], keep[:3], [1], [0])
+    Q, lse = rand(w.g, 3, 2, D), torch.empty(6, device="cuda")
+    out = torch.empty_like(Q)
+    refused(rv, INV, "not open", rv.attend_seqs, Q, None, None, pool, [gone], [3], out, lse)
+    refused(rv, INV, "both", rv.attend_seqs, Q, Q, None, pool, [a], [3], out, lse)
+    refused(rv, INV, "multiple of 2", rv.attend_seqs, Q[:, :1].contiguous(), None, None, pool, [a], [3],
+            out[:, :1].contiguous(), lse[:3])
+    with pytest.raises(ValueError, match="lse"):
+        rv.attend_seqs(Q, None, None, pool, [a], [3], out, lse[:5])
+    with pytest.raises(ValueError, match="shape"):
+        rv.attend_seqs(Q, None, None, pool, [a], [2], out, lse[:4])
+    with pytest.raises(ValueError, match="sequences"):
+        rv.attend_seqs(Q, None, None, pool, [a, b], [3], out, lse)
+    four = Q[None].expand(2, -1, -1, -1).contiguous()
+    sal, idx = torch.empty(2, 2, 3, device="cuda"), torch.empty(2, 2, 1, dtype=torch.int32, device="cuda")
+    refused(rv, INV, "named twice", rv.admit_seqs, four, four, four, sal, (1, 3, 0, 2), 1, pool, [a, a], sal, idx)
+    refused(rv, INV, "does not describe", rv.admit_seqs, four, four, four, sal, (1, 2, 0, 2), 1, pool, [a, b], sal, idx)
+    refused(rv, INV, "budget", rv.admit_seqs, four, four, four, sal, (1, 3, 0, 2), 4, pool, [a, b], sal,
+            torch.empty(2, 2, 4, dtype=torch.int32, device="cuda"))
+    assert pool.free_pages == free
+    w.verify()
+    for _ in range(2):  # what is left can still be opened and filled
+        w.open()
+    refused(rv, CAP, "open", pool.open)
+    w.append([a, b, c], [10, 10, 10])
+    w.verify()
+
+
+def test_a_pool_too_large_for_the_device(rv):
+    free = torch.cuda.mem_get_info()[0]
+    refused(rv, rv.RV_ERR_OOM, "pool allocation", rv.Pool, 1024, 1 << 30, 4, 1000)
+    assert abs(torch.cuda.mem_get_info()[0] - free) < 1 << 28
+    World(rv, 1, 2, 1, 10).open()
+
+
+def test_a_refused_stage_leaves_the_memory_alone(rv):
+    mem = rv.Memory(2, reserve_tokens=4, max_tokens=8)
+    prep = rv.QKVPrep(2, 2, norm="rms", axes=0)
+    x = torch.zeros(9, 128, dtype=torch.bfloat16, device="cuda")
+    Q = torch.zeros(9, 2, D, dtype=torch.bfloat16, device="cuda")
+    refused(rv, rv.RV_ERR_CAPACITY, "max_tokens", rv.stage_qkv, prep, x, x, x, None, Q, mem)
+    refused(rv, rv.RV_ERR_INVALID, "kv heads", rv.stage_qkv, rv.QKVPrep(2, 1, axes=0, norm=None), x, x[:, :64], x[:, :64],
+            None, Q, mem)
+    assert mem.len == 0 and mem.capacity == 4
+
+
+def test_tensors_of_another_device_are_refused(rv, monkeypatch):
+    w = World(rv, 2, 12, 5, 300)
+    a = w.open()
+    K = rand(w.g, 2, 2, D)
+    monkeypatch.setattr(rv, "_where", lambda stream: (1, 0))
+    with pytest.raises(ValueError, match="device 0 while device 1"):
+        w.pool.append([a], K, K, [2])
+    with pytest.raises(ValueError, match="device 0 while device 1"):
+        rv.attend_seqs(K, None, None, w.pool, [a], [2], K, torch.empty(4, device="cuda"))
+    prep = rv.QKVPrep(2, 2, norm=None, axes=0)
+    x = K.view(2, 128)
+    with pytest.raises(ValueError, match="device 0 while device 1"):
+        rv.prepare_qkv(prep, x, x, x, None, K, K, K)
+    assert w.pool.len(a) == 0
+
+
+class Index(int):
+    pass
+
+
+def test_plain_and_other_arguments_give_the_same(rv):
+    """What _rv_bind does not take (other integer types, bit views, subclasses) goes through ctypes."""
+    outs = []
+    for way in range(2):
+        w = World(rv, 2, 20, 6, 300, seed=3)
+        K, V = rand(w.g, 90, 2, D), rand(w.g, 90, 2, D)
+        if way:
+            class Sub(torch.Tensor):
+                pass
+            K, V = K.view(torch.int16), V.as_subclass(Sub)
+        num = Index if way else int
+        a = w.pool.open()
+        w.pool.append([num(a)], K, V, [num(90)])
+        kids = w.pool.fork(num(a), num(80), num(2))
+        w.pool.append(tuple(num(k) for k in kids), K[:5], V[:5], (num(2), num(3)))
+        Q = rand(gen(9), 4, 4, D)
+        out, lse = torch.empty_like(Q), torch.empty(16, device="cuda")
+        rv.attend_seqs(Q.view(torch.int16) if way else Q, None, None, w.pool, [num(k) for k in kids], [num(1), num(3)], out, lse)
+        keep = torch.tensor([[70, 1], [5, 5]], dtype=torch.int32, device="cuda")
+        w.pool.compact([num(kids[0])], keep, [num(2)], [num(1)])
+        got = torch.empty(6 + 166, D, dtype=torch.bfloat16, device="cuda")
+        w.pool.gather([num(k) for k in kids], got, None, [num(3), num(83)])
+        w.pool.release([num(kids[1])])
+        outs.append((out, lse, got, torch.tensor([w.pool.free_pages, *kids])))
+        prep = rv.QKVPrep(2, 1, norm="rms", axes=1, base=10000.0)
+        q, k, v = (rand(gen(s), 3, h * D) for s, h in ((1, 2), (2, 1), (3, 1)))
+        if way:
+            q, k, v = (t.view(torch.int16) for t in (q, k, v))
+        res = [torch.empty(3, h, D, dtype=torch.bfloat16, device="cuda") for h in (2, 1, 1)]
+        pos = torch.arange(3, dtype=torch.int32, device="cuda")
+        rv.prepare_qkv(prep, q, k, v, pos if way else pos[:, None], *res)
+        outs[-1] += tuple(res)
+    assert all(torch.equal(x, y) for x, y in zip(*outs))
+
+
+def test_two_graphs_share_the_workspace(rv):
+    w = World(rv, 2, 200, 20, 4000)
+    a = w.open()
+    w.append([a], [3000])
+    kids = w.fork(a, n=8)
+    w.append(kids, [5 * i for i in range(8)])
+    cases = []
+    for tokens in ([1] * 8, [40, 3, 0, 1, 1, 1, 1, 130]):
+        n = sum(tokens)
+        Q, K, V = (rand(w.g, n, 2, D) for _ in range(3))
+        out, lse = torch.empty_like(Q), torch.empty(2 * n, device="cuda")
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            rv.attend_seqs(Q, K, V, w.pool, kids, tokens, out, lse)
+        cases.append((g, tokens, Q, K, V, out, lse))
+    for rep in range(3):
+        for g, tokens, Q, K, V, out, lse in cases:
+            for t in (Q, K, V):
+                t.copy_(rand(w.g, *t.shape))
+            g.replay()
+            o2, l2 = torch.empty_like(out), torch.empty_like(lse)
+            rv.attend_seqs(Q, K, V, w.pool, kids, tokens, o2, l2)
+            torch.cuda.synchronize()
+            assert torch.equal(out, o2) and torch.equal(lse, l2)
+
+
+def test_rows_past_four_gigabytes(rv):
+    """2.5 million rows of 16 heads: 5.1 GB of keys, page offsets past 2^32 bytes."""
+    H, part, parts = 16, 500_000, 5
+    pool = rv.Pool(H, part * parts // 64 + 40, 4, part * parts + 64)
+    s = pool.open()
+    g = gen(11)
+    last = None
+    for i in range(parts):
+        K = torch.empty(part, H, D, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+        V = torch.empty(part, H, D, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+        pool.append([s], K, V, [part])
+        if i == parts - 1:
+            last = K, V
+        del K, V
+    n = part * parts
+    got = torch.empty(H, 100, D, dtype=torch.bfloat16, device="cuda")
+    pool.gather([s], None, got, [100], [n - 100])
+    assert torch.equal(got, last[1][-100:].transpose(0, 1))
+    keep = torch.randint(n - 5000, n, (H, 70), generator=g, device="cuda", dtype=torch.int32)
+    c = pool.fork(s, n)[0]
+    Q = rand(g, 2, H, D)
+    out, lse = torch.empty_like(Q), torch.empty(H, 2, device="cuda")
+    rv.attend_seqs(Q, None, None, pool, [c], [2], out, lse)
+    for h in (0, H - 1):
+        k, v = torch.empty(1, n, D, dtype=torch.bfloat16, device="cuda"), None
+        K = torch.empty(H, n, D, dtype=torch.bfloat16, device="cuda")
+        pool.gather([c], K, None, [n])
+        k = K[h].clone()
+        pool.gather([c], None, K, [n])
+        v = K[h].clone()
+        del K
+        z = Q[:, h].double() @ k.double().t() / 8
+        ref = torch.softmax(z, 1) @ v.double()
+        assert float((out[:, h].double() - ref).abs().max()) <= out_error_bound(ref.cpu().numpy(), float(v.abs().max()))
+        assert float((lse[h].double() - torch.logsumexp(z, 1)).abs().max()) <= LSE_ATOL
+    pool.compact([c], keep, [70])
+    got = torch.empty(H, 70, D, dtype=torch.bfloat16, device="cuda")
+    pool.gather([c], got, None, [70])
+    rows = (keep.long() - (n - part))[..., None].expand(-1, -1, D)
+    assert torch.equal(got, last[0].transpose(0, 1).gather(1, rows))
+    pool.close()
