@@ -381,7 +381,7 @@ rv_status rv_prepare_qkv_bwd(const rv_qkv_prep *p, const void *q, int64_t q_stri
 /* ---- sequences in pages ---------------------------------------------------------------
  *
  * A pool holds the rows of many sequences of one layer (streams, or continuations of one) in pages
- * of RV_PAGE_ROWS rows of every head, K and V [n_pages][n_heads][64][64] bf16.  A sequence is a
+ * of RV_PAGE_ROWS rows of every head, K and V [n_heads][n_pages][64][64] bf16.  A sequence is a
  * list of pages; forked sequences share pages, and a page returns to the pool when its last
  * user drops it.  Rows never move except in rv_pool_compact.  Lengths and lists are kept on the host
  * as enqueued (no device sync); the device's copy of the lists is written by kernels, in stream order.

@@ -29,7 +29,6 @@ __device__ __forceinline__ int last_at_or_below(int i0, int n, int x, F value) {
 struct SeqCursor {
   const char *pk, *pv;   // this head's rows of page 0
   const char *fk, *fv;   // this head's rows of the pass's first token
-  int64_t page_bytes;    // bytes between pages
   const int32_t* entry;  // the pass's table entries
   int n_pages, n_tiles;
   int last_rows, frame_rows;  // valid rows of the last page and of the last frame tile
@@ -75,7 +74,7 @@ struct TileOrder {
     r.last = (uint32_t)tc.valid(t) - 1;
     if (t < tc.n_pages) {  // uniform
       if (i - base >= 64) fetch(tc, i);
-      const int64_t at = (int64_t)__builtin_amdgcn_readlane(pages, i - base) * tc.page_bytes;
+      const int64_t at = (int64_t)__builtin_amdgcn_readlane(pages, i - base) * (TILE * 2);
       r.k = tc.pk + at;
       r.v = tc.pv + at;
       r.row = D * 2;
@@ -502,11 +501,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
                   ? nullptr
                   : a.part + (int64_t)seq_slot(p, shared, unit, c, uniform(seq_pos(p, unit, 0) / a.E)) * kSubFloats;
     SeqCursor tc;
-    tc.pk = reinterpret_cast<const char*>(a.pageK + (int64_t)g.h * TILE);
-    tc.pv = reinterpret_cast<const char*>(a.pageV + (int64_t)g.h * TILE);
+    tc.pk = reinterpret_cast<const char*>(a.pageK + (int64_t)g.h * a.n_pages * TILE);
+    tc.pv = reinterpret_cast<const char*>(a.pageV + (int64_t)g.h * a.n_pages * TILE);
     tc.fk = reinterpret_cast<const char*>(a.K + ((int64_t)p.tok0 * H + g.h) * D);
     tc.fv = reinterpret_cast<const char*>(a.V + ((int64_t)p.tok0 * H + g.h) * D);
-    tc.page_bytes = (int64_t)H * TILE * 2;
     tc.frame_row = 2u * (uint32_t)(H * D);
     tc.entry = a.table + p.entry0;
     tc.n_pages = p.n_pages;

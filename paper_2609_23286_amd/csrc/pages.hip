@@ -1,7 +1,9 @@
 // pages.hip -- rows into, out of and within the pages of a pool, gfx950.
 //
-// A page is 64 rows of every head, [H][64][64] bf16 for K and the same for V; a sequence's pages are
-// listed in its row of the device's page table.  All kernels here move 16-byte chunks, eight lanes to a
+// A page is 64 rows of every head; its rows of head h are [64][64] bf16 at page number `page` of the head's own
+// array, for K and the same for V ([H][n_pages][64][64]: with all heads of a page together, a head's pages would lie
+// a power of two apart and share a sixteenth of the L2's sets).  A sequence's pages are listed in its row of the
+// device's page table.  All kernels here move 16-byte chunks, eight lanes to a
 // row's 128 bytes, so that every access is whole cache lines whatever rows are picked; they are
 // bound by memory, and read and write past the caches' reuse (nontemporal: halving two memories of 52,000 rows
 // and reading them back 184 -> 163 us, at 5.2 TB/s).  A workgroup finds its sequence by its first-block number.
@@ -28,8 +30,8 @@ __device__ __forceinline__ int my_seq(const S* seq, int n) {
   return __builtin_amdgcn_readfirstlane(count - 1);
 }
 
-__device__ __forceinline__ int64_t page_at(int page, int H, int h, int row) {
-  return (((int64_t)page * H + h) * kPageRows + row) * D;
+__device__ __forceinline__ int64_t page_at(int page, int n_pages, int h, int row) {
+  return (((int64_t)h * n_pages + page) * kPageRows + row) * D;
 }
 
 __global__ __launch_bounds__(64) void table_kernel(TableArgs a) {
@@ -53,10 +55,10 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a) {
   if (r >= rows) return;
   const int i = skip + (int)(r / H), h = (int)(r % H), p = i / kPageRows;
   const int page = p == 0 ? s.page[0] : p == 1 || s.in_a_row ? s.page[1] + p - 1 : a.table[s.entry0 + p];
-  const int64_t to = page_at(page, H, h, i % kPageRows) + e;
+  const int64_t to = page_at(page, a.n_pages, h, i % kPageRows) + e;
   u32x4 k, v;
   if (i < s.offset) {
-    const int64_t from = page_at(s.cow, H, h, i) + e;
+    const int64_t from = page_at(s.cow, a.n_pages, h, i) + e;
     k = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.K + from));
     v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.V + from));
   } else {
@@ -82,7 +84,7 @@ __global__ __launch_bounds__(NT) void gather_kernel(GatherArgs a) {
   const int e = 8 * (threadIdx.x & 7);
   if (r >= (int64_t)s.n * H) return;
   const int h = (int)(r / s.n), i = s.offset + (int)(r - (int64_t)h * s.n);
-  const int64_t from = page_at(a.table[s.entry0 + i / kPageRows], H, h, i % kPageRows) + e;
+  const int64_t from = page_at(a.table[s.entry0 + i / kPageRows], a.n_pages, h, i % kPageRows) + e;
   const int64_t to = (s.dst_row + r) * D + e;
   if (a.dstK) __builtin_nontemporal_store(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.K + from)), reinterpret_cast<u32x4*>(a.dstK + to));
   if (a.dstV) __builtin_nontemporal_store(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.V + from)), reinterpret_cast<u32x4*>(a.dstV + to));
@@ -107,12 +109,12 @@ __global__ __launch_bounds__(NT) void compact_kernel(CompactArgs a) {
   }
   u32x4 k = {0, 0, 0, 0}, v = k;
   if (row >= 0) {
-    const int64_t from = page_at(a.table[s.old0 + row / kPageRows], H, h, row % kPageRows) + e;
+    const int64_t from = page_at(a.table[s.old0 + row / kPageRows], a.n_pages, h, row % kPageRows) + e;
     k = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.K + from));
     v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.V + from));
   }
   const int page = s.page0 >= 0 ? s.page0 + i / kPageRows : a.table[s.new0 + i / kPageRows];
-  const int64_t to = page_at(page, H, h, i % kPageRows) + e;
+  const int64_t to = page_at(page, a.n_pages, h, i % kPageRows) + e;
   __builtin_nontemporal_store(k, reinterpret_cast<u32x4*>(a.K + to));
   __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(a.V + to));
 }

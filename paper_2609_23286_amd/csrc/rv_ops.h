@@ -81,13 +81,13 @@ struct AppendSeq {
 };
 constexpr int kMaxAppend = 64;
 struct AppendArgs {
-  uint16_t *K, *V;    // pages [n_pages][H][64][64]
+  uint16_t *K, *V;    // pages [H][n_pages][64][64]
   int32_t* table;
   const uint16_t *srcK, *srcV;  // row j of head h: src + (src_row + j) H 64 + h 64
   const int32_t* idx;           // NULL, or per sequence [H][n]: row j of head h is frame token
                                 //   idx[h][j] (sequence i's block starts at H src_row)
   int idx_tokens;               // ... of a frame of this many tokens, sequence i's at i idx_tokens
-  int n_heads, n_seqs, blocks;
+  int n_heads, n_pages, n_seqs, blocks;
   AppendSeq seq[kMaxAppend];
 };
 
@@ -104,7 +104,7 @@ struct GatherArgs {
   const uint16_t *K, *V;
   const int32_t* table;
   uint16_t *dstK, *dstV;  // either may be NULL
-  int n_heads, n_seqs, blocks;
+  int n_heads, n_pages, n_seqs, blocks;
   GatherSeq seq[kMaxGather];
 };
 
@@ -127,7 +127,7 @@ struct CompactArgs {
   uint16_t *K, *V;
   int32_t* table;
   const int32_t* keep;
-  int n_heads, n_seqs, blocks;
+  int n_heads, n_pages, n_seqs, blocks;
   CompactSeq seq[kMaxCompact];
 };
 
@@ -222,12 +222,12 @@ constexpr int kSubsPerTile = kAttnBQ / kSubRows;
 constexpr int kMergeOne = 4, kMergeFew = 16;  // rows a merge workgroup takes: a wave one, or four
 struct SeqArgs {
   const uint16_t *Q, *K, *V;      // packed frames [tokens][Hq or H][64]; K, V NULL without frame keys
-  const uint16_t *pageK, *pageV;  // [n_pages][H][64][64]
+  const uint16_t *pageK, *pageV;  // [H][n_pages][64][64]
   const int32_t* table;
   uint16_t* out;
   float* lse;
   float* part;
-  int n_heads, group;             // kv heads, query heads to each
+  int n_heads, n_pages, group;    // kv heads, pages of the pool, query heads to each kv head
   int n_pass, n_inner;            // passes; the first n_inner are not leaves
   int total, E, chunks;           // positions, positions a chunk, chunks
   int inner_chunks;               // chunks that begin in an inner pass

@@ -9,7 +9,7 @@
 
 struct rv_pool_s {
   int device = 0;
-  int n_heads = 0;
+  int n_heads = 0, n_pages = 0;
   int64_t max_rows = 0;
   uint16_t* K = nullptr;
   uint16_t* V = nullptr;
@@ -112,6 +112,7 @@ rv_status append(rv_pool p, int n, const int* seqs, const void* K, const void* V
   a.idx = idx;
   a.idx_tokens = idx_tokens;
   a.n_heads = p->n_heads;
+  a.n_pages = p->n_pages;
   Runs runs(p, s);
   hipError_t err = hipSuccess;
   auto flush = [&]() {
@@ -172,6 +173,7 @@ rv_status rv_pool_create(int n_heads, int head_dim, int n_pages, int max_seqs, i
   rv_pool p = new (std::nothrow) rv_pool_s;
   if (!p) return fail(RV_ERR_OOM, "host allocation failed");
   p->n_heads = n_heads;
+  p->n_pages = n_pages;
   p->max_rows = max_rows;
   const size_t bytes = (size_t)n_pages * n_heads * kPageRows * rv::kHeadDim * 2;
   hipError_t e = hipGetDevice(&p->device);
@@ -315,6 +317,7 @@ rv_status rv_pool_gather(rv_pool p, int n, const int* seqs, const int64_t* first
   a.dstK = (uint16_t*)K;
   a.dstV = (uint16_t*)V;
   a.n_heads = p->n_heads;
+  a.n_pages = p->n_pages;
   int64_t dst_row = 0;
   for (int i = 0; i < n; ++i) {
     if (n_rows[i] == 0) continue;
@@ -363,6 +366,7 @@ rv_status rv_pool_compact(rv_pool p, int n, const int* seqs, const int64_t* firs
   a.table = p->table;
   a.keep = keep;
   a.n_heads = p->n_heads;
+  a.n_pages = p->n_pages;
   Runs runs(p, s);
   hipError_t err = hipSuccess;
   auto flush = [&]() {
@@ -442,6 +446,7 @@ rv_status rv_attend_seqs(rv_pool p, int n, const int* seqs, const int* n_tokens,
   a.lse = lse;
   a.part = ctx.seq_part;
   a.n_heads = p->n_heads;
+  a.n_pages = p->n_pages;
   a.group = n_q_heads / p->n_heads;
   a.n_queues = ctx.n_queues;
   int tok0 = 0;
