@@ -56,17 +56,21 @@ struct TileRows {
                   // and a weight of zero makes zero only of numbers)
 };
 
-// The tiles a wave loads, in turn: index i is tile first + i step.  Their page numbers are held a lane
-// each and fetched 64 at a time, so that no tile's addresses wait for memory (a scalar load of the entry
-// for each tile cost a tenth of the forward launch).
+// The tiles a wave loads, in turn: index i is tile first + i step (modulo the segment).  Their page numbers are
+// held a lane each and fetched 64 at a time, so that no tile's addresses wait for memory (a scalar load of the
+// entry for each tile cost a tenth of the forward launch).
 struct TileOrder {
   int first, step;
+  int up, wrap;   // indices from `up` on go back by `wrap` tiles
   int base = 0;   // index of lane 0's page
   int pages;      // this lane's page number
-  __device__ __forceinline__ int at(int i) const { return first + i * step; }
+  __device__ __forceinline__ int at(int i) const { return first + i * step - (i >= up ? wrap : 0); }
   __device__ __forceinline__ void fetch(const SeqCursor& tc, int i) {
     base = i;
-    pages = tc.n_pages > 0 ? tc.entry[min(at(i + (int)(threadIdx.x & 63)), tc.n_pages - 1)] : 0;
+    pages = tc.n_pages > 0 ? tc.entry[max(0, min(at(i + (int)(threadIdx.x & 63)), tc.n_pages - 1))] : 0;
+    // (Read here, so that the wait for it stands here: at its use the compiler would wait, for every tile, for all
+    // the loads of the tiles before: 3 % of a frame over 52,000 rows.)
+    asm volatile("" : "+v"(pages));
   }
   __device__ __forceinline__ TileRows rows(const SeqCursor& tc, int i) {
     const int t = at(i);
@@ -317,9 +321,9 @@ __device__ __forceinline__ void write_row(const SeqArgs& a, const SeqPass& p, in
   }
 }
 
-// A segment: tiles t0 .. t1 - 1 of one unit.
+// A segment: tiles t0 .. t1 - 1 of one unit, taken in the order ts .. t1 - 1, t0 .. ts - 1.
 struct Segment {
-  int h, qt, t0, t1;
+  int h, qt, t0, t1, ts;
   float* slots;   // partial slots of the segment, or NULL: it is the whole unit, and final
 };
 
@@ -347,7 +351,7 @@ __device__ __forceinline__ void narrow_segment(const SeqArgs& a, const SeqPass& 
   const uint16_t* const st0 = lds + wave * 2 * kHalfStage;
   const uint16_t* const st1 = st0 + kHalfStage;
   const int n = g.t1 - g.t0 > wave ? (g.t1 - g.t0 - wave + 3) / 4 : 0;  // tiles of this wave
-  TileOrder order{g.t0 + wave, 4};
+  TileOrder order{g.t0 + wave, 4, 1 << 30, 0};
   TileRows next{};
   if (n > 0) {
     order.fetch(tc, 0);
@@ -418,30 +422,31 @@ __device__ __forceinline__ void wide_segment(const SeqArgs& a, const SeqPass& p,
   sm.o0 = f32x16{};
   sm.o1 = f32x16{};
   const bool active = q0 < rows;
-  TileOrder order{t0, 1};
+  const int n = t1 - t0;
+  TileOrder order{g.ts, 1, t1 - g.ts, n};
   order.fetch(tc, 0);
   const uint32_t ring = (uint32_t)(uintptr_t)(lds_void*)lds + wave * 8 * D * 2;
   constexpr uint32_t kStageBytes = STAGE * 2;
   load_tile(order.rows(tc, 0), ring);
-  if (t0 + 1 < t1) load_tile(order.rows(tc, 1), ring + kStageBytes);
+  if (n > 1) load_tile(order.rows(tc, 1), ring + kStageBytes);
   // (the queries pass through the wait: the compiler's own for them would wait for tiles in the loop)
   asm volatile("s_waitcnt vmcnt(0)" : "+v"(qf[0]), "+v"(qf[1]), "+v"(qf[2]), "+v"(qf[3])::"memory");
   __syncthreads();
-  auto step = [&](auto phase, int t) {
+  auto step = [&](auto phase, int i) {
     constexpr int P = decltype(phase)::value;
-    if (t + 2 < t1) load_tile(order.rows(tc, t + 2 - t0), ring + (P + 2) % NSTAGE * kStageBytes);
-    if (t + 3 < t1) load_tile(order.rows(tc, t + 3 - t0), ring + (P + 3) % NSTAGE * kStageBytes);
-    if (active && t + 1 < t1)
-      compute_pair(lds + P * STAGE, lds + (P + 1) * STAGE, qf, lane, tc.valid(t), tc.valid(t + 1), sm);
+    if (i + 2 < n) load_tile(order.rows(tc, i + 2), ring + (P + 2) % NSTAGE * kStageBytes);
+    if (i + 3 < n) load_tile(order.rows(tc, i + 3), ring + (P + 3) % NSTAGE * kStageBytes);
+    if (active && i + 1 < n)
+      compute_pair(lds + P * STAGE, lds + (P + 1) * STAGE, qf, lane, tc.valid(order.at(i)), tc.valid(order.at(i + 1)), sm);
     else if (active)
-      compute<2>(lds + P * STAGE, lds + P * STAGE + TILE, qf, lane, tc.valid(t), sm);
+      compute<2>(lds + P * STAGE, lds + P * STAGE + TILE, qf, lane, tc.valid(order.at(i)), sm);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
-  for (int t = t0; t < t1; t = uniform(t + 4)) {
-    step(StageConst<0>{}, t);
-    if (t + 2 >= t1) break;
-    step(StageConst<2>{}, t + 2);
+  for (int i = 0; i < n; i = uniform(i + 4)) {
+    step(StageConst<0>{}, i);
+    if (i + 2 >= n) break;
+    step(StageConst<2>{}, i + 2);
   }
 
   // Rows through LDS, so that whole rows are written (the ring is free: the last step ended in a barrier).
@@ -475,31 +480,17 @@ __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
   __shared__ float s_m[4][kSubRows], s_l[4][kSubRows];
   const int c = uniform(seq_chunk_of(a, (int)blockIdx.x));
   if (c < 0) return;
-  const int begin = c * a.E, end = min(begin + a.E, a.total);
-  int ip = last_at_or_below(0, a.n_pass, begin, [&](int i) { return a.pos0[i]; });
-  for (int pos = begin; pos < end;) {  // pos: the chunk's positions from here on are still to be done
+  const int H = a.n_heads;
+  int done = 0;  // tiles this workgroup has taken
+  auto run = [&](int ip, int unit, int T, int t0, int t1, float* slots) {
     const SeqPass& p = a.pass[ip];
-    const int H = a.n_heads, T = seq_tiles(p), units = H * p.q_tiles;
     Segment g;
-    int unit = 0;
-    g.t0 = T == 0 ? 0 : uniform(seq_first_tile(p, T, pos - p.pos0, &unit));
-    unit = uniform(unit);
-    if (T == 0 || unit >= units) {
-      if (++ip >= a.n_pass) break;
-      pos = max(pos, a.pos0[ip]);  // (the chunk may begin inside the last tile before it)
-      continue;
-    }
-    int end_unit = 0;
-    const int end_tile = uniform(seq_first_tile(p, T, end - p.pos0, &end_unit));
-    g.t1 = uniform(end_unit) > unit ? T : end_tile;
-    if (uniform(end_unit) < unit || g.t1 <= g.t0) break;  // the last positions belong to a tile that began before
+    g.t0 = t0;
+    g.t1 = t1;
+    g.slots = slots;
     // query tiles of a head are neighbours
     g.h = uniform(unit / p.q_tiles);
     g.qt = unit - g.h * p.q_tiles;
-    const bool shared = ip < a.n_inner || p.parent >= 0;
-    g.slots = !shared && g.t0 == 0 && g.t1 == T
-                  ? nullptr
-                  : a.part + (int64_t)seq_slot(p, shared, unit, c, uniform(seq_pos(p, unit, 0) / a.E)) * kSubFloats;
     SeqCursor tc;
     tc.pk = reinterpret_cast<const char*>(a.pageK + (int64_t)g.h * a.n_pages * TILE);
     tc.pv = reinterpret_cast<const char*>(a.pageV + (int64_t)g.h * a.n_pages * TILE);
@@ -511,11 +502,53 @@ __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
     tc.n_tiles = T;
     tc.last_rows = p.last_rows;
     tc.frame_rows = p.frame > 0 ? p.frame - (T - p.n_pages - 1) * BK : p.last_rows;
-    if (p.tile_rows == kSubRows)
+    if (p.tile_rows == kSubRows) {
       narrow_segment(a, p, tc, g, lds, s_m, s_l);
-    else
+    } else {
+      // The sums over a segment's keys take any order.  The chunks of a head cover different keys; the one that has
+      // worked for i tiles takes tile i modulo the chunk's length where its segment holds it, so that they are at the
+      // same few tiles at a time and find them in their XCD's L2.  (In key order each fetched its keys from beyond
+      // it, and that was the bound: 1041 queries over 52,000 rows 342 -> 322 us.)
+      const int per = uniform(max(1, a.E / p.cost));
+      const int ahead = uniform((done - t0) % per);
+      g.ts = t0 + (ahead < 0 ? ahead + per : ahead);
+      if (g.ts >= t1) g.ts = t0;
       wide_segment(a, p, tc, g, lds, s_m, s_l);
-    pos = g.t1 < T ? end : seq_pos(p, unit + 1, 0);
+    }
+    done += t1 - t0;
+  };
+  for (int r = 0; r < a.rounds && c < a.width; ++r) {
+    const int u = uniform(r * a.width + c);
+    const int ip = last_at_or_below(0, a.n_pass, u, [&](int i) { return a.unit0[i]; });
+    const int T = seq_tiles(a.pass[ip]);
+    run(ip, u - a.unit0[ip], T, 0, T, nullptr);
+  }
+  if (c >= a.chunks) return;
+  const int begin = a.pos_first + c * a.E, end = min(begin + a.E, a.total);
+  done = 0;
+  int ip = last_at_or_below(0, a.n_pass, begin, [&](int i) { return a.pos0[i]; });
+  for (int pos = begin; pos < end;) {  // pos: the chunk's positions from here on are still to be done
+    const SeqPass& p = a.pass[ip];
+    const int T = seq_tiles(p), units = H * p.q_tiles;
+    int unit = 0;
+    const int t0 = T == 0 ? 0 : uniform(seq_first_tile(p, T, pos - p.pos0, &unit));
+    unit = uniform(unit);
+    if (T == 0 || unit >= units) {
+      if (++ip >= a.n_pass) break;
+      pos = max(pos, a.pos0[ip]);  // (the chunk may begin inside the last tile before it)
+      continue;
+    }
+    int end_unit = 0;
+    const int end_tile = uniform(seq_first_tile(p, T, end - p.pos0, &end_unit));
+    const int t1 = uniform(end_unit) > unit ? T : end_tile;
+    if (uniform(end_unit) < unit || t1 <= t0) break;  // the last positions belong to a tile that began before
+    const bool shared = ip < a.n_inner || p.parent >= 0;
+    float* const slots = !shared && t0 == 0 && t1 == T
+                             ? nullptr
+                             : a.part + (int64_t)seq_slot(p, shared, unit, c, uniform(seq_chunk_at(a, seq_pos(p, unit, 0)))) *
+                                            kSubFloats;
+    run(ip, unit, T, t0, t1, slots);
+    pos = t1 < T ? end : seq_pos(p, unit + 1, 0);
   }
 }
 
@@ -547,7 +580,9 @@ __device__ __forceinline__ void merge_rows(const SeqArgs& a, const SeqPass& leaf
       if (T == 0) continue;
       const int r = (leaf.tok0 - p.tok0) * G + row;
       const int qt = uniform(r / p.tile_rows), unit = h * p.q_tiles + qt;
-      const int c0 = uniform(seq_pos(p, unit, 0) / a.E), n = uniform(seq_pos(p, unit, T - 1) / a.E) - c0 + 1;  // its chunks
+      if (seq_whole(a, p, unit)) return;  // written by the forward launch
+      const int c0 = uniform(seq_chunk_at(a, seq_pos(p, unit, 0)));
+      const int n = uniform(seq_chunk_at(a, seq_pos(p, unit, T - 1))) - c0 + 1;  // its chunks
       if (!shared && n == 1) return;  // written by the forward launch
       stride[k] = seq_slot_step(p, shared);
       first[k] = seq_slot(p, shared, unit, c0, c0) + r % p.tile_rows / kSubRows - count[k] * stride[k];
@@ -628,7 +663,7 @@ __global__ __launch_bounds__(256) void seq_merge_kernel(SeqArgs a) {
 }  // namespace
 
 hipError_t launch_attend_seqs(const SeqArgs& a, hipStream_t s) {
-  if (a.chunks > 0) {
+  if (seq_grid(a) > 0) {
     hipLaunchKernelGGL(seq_fwd_kernel, dim3((unsigned)seq_grid(a)), dim3(kAttnThreads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -198,10 +198,14 @@ class PageBook {
 // context is its own pass (a leaf) and the passes above it.
 //
 // A unit is one query tile of one kv head of a pass; its work is the pass's key tiles, each of
-// `cost` positions, and `fixed` more before its second.  The positions of all units, one after another, are cut into chunks of E, one
-// workgroup each: a tile belongs to the chunk that its first position lies in.
+// `cost` positions, and `fixed` more before its second.  Units are numbered through all passes.  Where they are
+// alike and more than the device's workgroup slots, the first `rounds` times `width` are dealt out whole, one of a
+// round to each workgroup, so that neighbours (query tiles of a head) go over the same keys at the same time.
+// The positions of the others, one unit after another from pos_first on, are cut into chunks of E, one workgroup
+// each: a tile belongs to the chunk that its first position lies in.
 struct SeqPass {
   int32_t pos0;       // first position
+  int32_t unit0;      // first unit
   int32_t tok0, n_tok;
   int32_t entry0;     // table entry of the first page
   int32_t n_pages;
@@ -215,7 +219,7 @@ struct SeqPass {
   int32_t slot0;      // shared passes (inner ones, and leaves below one): slot of unit 0 and chunk 0
   int32_t merge_rows; // leaves: rows a merge workgroup takes
 };
-constexpr int kMaxPasses = 56;
+constexpr int kMaxPasses = 52;
 constexpr int kSubRows = 32;  // rows of a partial slot of this launch
 constexpr int kSubFloats = kSubRows * kHeadDim + 2 * kSubRows;  // fp32 rows, references, row sums
 constexpr int kSubsPerTile = kAttnBQ / kSubRows;
@@ -229,11 +233,13 @@ struct SeqArgs {
   float* part;
   int n_heads, n_pages, group;    // kv heads, pages of the pool, query heads to each kv head
   int n_pass, n_inner;            // passes; the first n_inner are not leaves
-  int total, E, chunks;           // positions, positions a chunk, chunks
+  int rounds, width;              // whole units to a workgroup, and workgroups that take them
+  int pos_first, total, E, chunks;  // positions of the units that are cut: [pos_first, total), chunks of E
   int inner_chunks;               // chunks that begin in an inner pass
   int n_queues;                   // XCDs that the workgroups are dealt over
   int merge_blocks;
-  int32_t pos0[kMaxPasses];    // the passes' first positions, again (a workgroup finds its pass by them)
+  int32_t pos0[kMaxPasses];    // the passes' first positions and units, again (a workgroup finds its pass by them)
+  int32_t unit0[kMaxPasses];
   int32_t merge0[kMaxPasses];  // leaves: first workgroup of the merge launch
   SeqPass pass[kMaxPasses];
 };
@@ -251,13 +257,14 @@ RV_HD inline int seq_first_tile(const SeqPass& p, int T, int off, int* unit) {
   *unit = t < T ? u : u + 1;
   return t < T ? t : 0;
 }
-// The chunk of a workgroup, or -1.  Workgroups are dealt to the XCDs in turn; consecutive chunks (query
+// The chunk (and place in a round) of a workgroup, or -1.  Workgroups are dealt to the XCDs in turn; consecutive chunks (query
 // tiles of a head) go to one XCD, and each XCD gets its share of the inner passes' chunks, which are
 // bound by arithmetic, and of the leaves', which are bound by memory.
 RV_HD inline int seq_share(int n, int x, int X) { return (int)((int64_t)n * x / X); }
 template <class A>
 RV_HD inline int seq_chunk_of(const A& a, int block) {
-  const int X = a.n_queues, x = block % X, rest = a.chunks - a.inner_chunks;
+  const int X = a.n_queues, x = block % X, all = a.rounds > 0 && a.width > a.chunks ? a.width : a.chunks;
+  const int rest = all - a.inner_chunks;
   int j = block / X;
   const int i0 = seq_share(a.inner_chunks, x, X), ni = seq_share(a.inner_chunks, x + 1, X) - i0;
   if (j < ni) return i0 + j;
@@ -267,9 +274,15 @@ RV_HD inline int seq_chunk_of(const A& a, int block) {
 }
 template <class A>
 RV_HD inline int seq_grid(const A& a) {
-  const int X = a.n_queues;
-  return X * ((a.inner_chunks + X - 1) / X + (a.chunks - a.inner_chunks + X - 1) / X);
+  const int X = a.n_queues, all = a.rounds > 0 && a.width > a.chunks ? a.width : a.chunks;
+  return X * ((a.inner_chunks + X - 1) / X + (all - a.inner_chunks + X - 1) / X);
 }
+
+template <class A>
+RV_HD inline int seq_chunk_at(const A& a, int pos) { return (pos - a.pos_first) / a.E; }
+// Whether a unit was dealt out whole.
+template <class A>
+RV_HD inline bool seq_whole(const A& a, const SeqPass& p, int unit) { return p.unit0 + unit < a.rounds * a.width; }
 
 // Partial slot of the segment of unit `unit` that chunk c takes, where c0 is the unit's first chunk.
 // Shared passes: a slot for each unit and chunk (their sum grows with each segment).  Other

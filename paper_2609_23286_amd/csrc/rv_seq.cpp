@@ -287,46 +287,72 @@ int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool 
     a->n_inner = b.n_inner;
     a->n_pass = b.n_inner + b.n_leaf;
     std::copy(b.leaf, b.leaf + b.n_leaf, a->pass + b.n_inner);
-    int64_t pos = 0;
-    bool fits = true;
+    int64_t pos = 0, units = 0;
+    int64_t longest = 0, shortest = INT64_MAX;  // positions of a unit
+    bool fits = true, alike = a->n_inner == 0;
     for (int i = 0; i < a->n_pass; ++i) {
       SeqPass& p = a->pass[i];
-      const bool narrow = p.tile_rows < kAttnBQ;
+      const bool narrow = p.tile_rows == kSubRows;
+      const int64_t T = seq_tiles(p);
       p.cost = narrow ? kNarrowCost : kWideCost;
-      p.fixed = seq_tiles(p) == 0 ? 0 : narrow ? kNarrowFixed : kWideFixed;
+      p.fixed = T == 0 ? 0 : narrow ? kNarrowFixed : kWideFixed;
       a->pos0[i] = p.pos0 = (int)std::min<int64_t>(pos, INT32_MAX);
-      pos += (int64_t)p.q_tiles * n_heads * (p.fixed + (int64_t)seq_tiles(p) * p.cost);
+      a->unit0[i] = p.unit0 = (int)std::min<int64_t>(units, INT32_MAX);
+      const int64_t per = p.fixed + T * p.cost;
+      pos += (int64_t)p.q_tiles * n_heads * per;
+      units += (int64_t)p.q_tiles * n_heads;
+      longest = std::max(longest, per);
+      shortest = std::min(shortest, per);
+      alike = alike && !narrow;
     }
-    if (pos > INT32_MAX / 2) {
+    if (pos > INT32_MAX / 2 || units > INT32_MAX / 2) {
       if (n == 1) return 0;
       continue;
     }
-    // Chunks of equal length, one for each of the device's workgroup slots, but no shorter than
-    // kMinChunk.  (With inner passes an XCD's two shares are rounded up each: a workgroup more than its
-    // slots would wait for a whole chunk.)
+    alike = alike && shortest > 0 && longest * 4 <= shortest * 5;
+    // The device's workgroup slots.  (With inner passes an XCD's two shares are rounded up each: a workgroup more
+    // than its slots would wait for a whole chunk.)
+    const int at_once = std::max(1, kAttnWgPerCu * n_cus - (a->n_inner > 0 ? a->n_queues : 0));
     a->total = (int)pos;
-    const int slots_at_once = std::max(1, kAttnWgPerCu * n_cus - (a->n_inner > 0 ? a->n_queues : 0));
-    a->E = (int)std::max<int64_t>(kMinChunk, ceil_div64(pos, slots_at_once));
-    a->chunks = (int)ceil_div64(pos, a->E);
+    a->pos_first = 0;
+    a->rounds = alike ? (int)(units / at_once) : 0;
+    a->width = at_once;
+    if (a->rounds > 0) {
+      const int first = a->rounds * at_once;  // the first unit that is cut
+      int i = a->n_pass - 1;
+      while (i > 0 && a->unit0[i] > first) --i;
+      a->pos_first = first < units ? seq_pos(a->pass[i], first - a->unit0[i], 0) : a->total;
+      units -= first;
+    }
+    // Chunks of equal length, one for each slot, but no shorter than kMinChunk.  Units of one length are cut into equal
+    // pieces instead where that takes no longer than a second unit's start would.
+    const int64_t rest = a->total - a->pos_first;
+    a->E = (int)std::max<int64_t>(kMinChunk, ceil_div64(rest, at_once));
+    if (alike && longest == shortest && units > 0 && units <= at_once) {
+      const int64_t piece = ceil_div64(longest, at_once / units);
+      if (piece >= kMinChunk && piece <= a->E + kWideFixed) a->E = (int)ceil_div64(longest, ceil_div64(longest, piece));
+    }
+    a->chunks = (int)ceil_div64(rest, a->E);
     const int leaf0 = a->n_inner < a->n_pass ? a->pass[a->n_inner].pos0 : a->total;
     a->inner_chunks = (int)ceil_div64(leaf0, a->E);
     int64_t slots = (2 * (int64_t)a->chunks + 1) * kSubsPerTile, merge = 0;
     for (int i = 0; i < a->n_pass; ++i) {
       SeqPass& p = a->pass[i];
-      const int units = p.q_tiles * n_heads, T = seq_tiles(p);
+      const int n_units = p.q_tiles * n_heads, T = seq_tiles(p);
       const bool leaf = i >= a->n_inner, shared = !leaf || p.parent >= 0;
       if (shared && T > 0) {
-        const int first = p.pos0 / a->E, last = seq_pos(p, units - 1, T - 1) / a->E;
+        const int first = seq_chunk_at(*a, p.pos0), last = seq_chunk_at(*a, seq_pos(p, n_units - 1, T - 1));
         p.slot0 = (int)(slots - (int64_t)first * (p.tile_rows / kSubRows));
-        slots += (int64_t)(units + last - first) * (p.tile_rows / kSubRows);
+        slots += (int64_t)(n_units + last - first) * (p.tile_rows / kSubRows);
         fits = fits && slots <= max_slots;
       }
       a->merge0[i] = (int)merge;
       if (!leaf) continue;
       // merged: sums in parts, or none at all
       int most = T == 0 ? 2 : 1;
-      for (int u = 0; u < units && T > 0; ++u)
-        most = std::max(most, seq_pos(p, u, T - 1) / a->E - seq_pos(p, u, 0) / a->E + 1);
+      for (int u = 0; u < n_units && T > 0; ++u)
+        if (!seq_whole(*a, p, u))
+          most = std::max(most, seq_chunk_at(*a, seq_pos(p, u, T - 1)) - seq_chunk_at(*a, seq_pos(p, u, 0)) + 1);
       p.merge_rows = shared || most > kFewSegments ? kMergeOne : kMergeFew;
       if (shared || most > 1) merge += ceil_div64((int64_t)p.n_tok * group, p.merge_rows) * n_heads;
     }

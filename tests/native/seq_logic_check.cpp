@@ -156,7 +156,8 @@ struct World {
                                      uniform(1, 300), max_slots, &a);
       CHECK(done >= 1 && done <= (int)(span.size() - i), "sequences covered");
       CHECK(a.n_pass <= rv::kMaxPasses && a.n_pass - a.n_inner == done, "passes");
-      CHECK(a.E > 0 && (int64_t)a.chunks * a.E >= a.total && (int64_t)(a.chunks - 1) * a.E < a.total, "chunks");
+      CHECK(a.E > 0 && (int64_t)a.chunks * a.E >= a.total - a.pos_first &&
+                (a.chunks == 0 || (int64_t)(a.chunks - 1) * a.E < a.total - a.pos_first), "chunks");
       // the segments, as the kernel walks them
       std::set<std::vector<int>> tiles_done;
       std::map<int, std::vector<int>> slot_of;       // sub-slot -> pass, unit
@@ -171,10 +172,21 @@ struct World {
         if (rv::seq_chunk_of(a, b) >= 0) order.push_back(rv::seq_chunk_of(a, b));
       std::vector<int> sorted = order;
       std::sort(sorted.begin(), sorted.end());
-      for (int c = 0; c < a.chunks; ++c) CHECK(c < (int)sorted.size() && sorted[c] == c, "chunk %d", c);
-      CHECK((int)sorted.size() == a.chunks, "chunks taken");
+      const int places = a.rounds > 0 ? std::max(a.width, a.chunks) : a.chunks;
+      for (int c = 0; c < places; ++c) CHECK(c < (int)sorted.size() && sorted[c] == c, "chunk %d", c);
+      CHECK((int)sorted.size() == places, "chunks taken");
       for (int c : order) {
-        const int begin = c * a.E, end = std::min(begin + a.E, a.total);
+        for (int r = 0; r < a.rounds && c < a.width; ++r) {
+          int ip = -1;
+          while (ip + 1 < a.n_pass && a.unit0[ip + 1] <= r * a.width + c) ++ip;
+          const rv::SeqPass& p = a.pass[ip];
+          const int unit = r * a.width + c - a.unit0[ip];
+          CHECK(unit < n_heads * p.q_tiles && ip >= a.n_inner && p.parent < 0, "a unit of no pass");
+          for (int t = 0; t < rv::seq_tiles(p); ++t) CHECK(tiles_done.insert({ip, unit, t}).second, "a tile taken twice");
+          segments[{ip, unit, -1}] = -1;
+        }
+        if (c >= a.chunks) continue;
+        const int begin = a.pos_first + c * a.E, end = std::min(begin + a.E, a.total);
         int ip = last_below(begin);
         for (int pos = begin; pos < end;) {
           const rv::SeqPass& p = a.pass[ip];
@@ -193,11 +205,11 @@ struct World {
           CHECK(t0 >= 0 && t0 < t1 && unit >= 0 && unit < units, "a segment outside its unit");
           for (int t = t0; t < t1; ++t) {
             CHECK(tiles_done.insert({ip, unit, t}).second, "a tile taken twice");
-            CHECK(rv::seq_pos(p, unit, t) / a.E == c, "a tile of another chunk");
+            CHECK(rv::seq_chunk_at(a, rv::seq_pos(p, unit, t)) == c, "a tile of another chunk");
           }
           int slot = -1;
           if (shared || t0 > 0 || t1 < T) {
-            slot = rv::seq_slot(p, shared, unit, c, rv::seq_pos(p, unit, 0) / a.E);
+            slot = rv::seq_slot(p, shared, unit, c, rv::seq_chunk_at(a, rv::seq_pos(p, unit, 0)));
             for (int q = slot; q < slot + p.tile_rows / rv::kSubRows; ++q) {
               CHECK(q >= 0 && (q < max_slots || done == 1), "slot %d", q);
               CHECK(slot_of.emplace(q, std::vector<int>{ip, unit, c}).second, "slot %d used twice", q);
@@ -207,11 +219,13 @@ struct World {
           pos = t1 < T ? end : rv::seq_pos(p, unit + 1, 0);
         }
       }
-      int merge = 0, pos = 0;
+      int merge = 0, pos = 0, all_units = 0;
       for (int k = 0; k < a.n_pass; ++k) {
         const rv::SeqPass& p = a.pass[k];
         const int T = rv::seq_tiles(p), units = n_heads * p.q_tiles;
         CHECK(p.pos0 == pos && a.pos0[k] == pos && p.cost > 0, "first position");
+        CHECK(p.unit0 == all_units && a.unit0[k] == all_units, "first unit");
+        all_units += units;
         pos += units * (p.fixed + T * p.cost);
         CHECK((int64_t)p.q_tiles * p.tile_rows >= (int64_t)p.n_tok * group, "query tiles");
         CHECK(p.parent < a.n_inner && (k < a.n_inner ? p.parent < k : true), "parent");
@@ -221,7 +235,12 @@ struct World {
           if (T == 0) continue;
           // as the merge finds them
           const bool shared = k < a.n_inner || p.parent >= 0;
-          const int c0 = rv::seq_pos(p, u, 0) / a.E, n = rv::seq_pos(p, u, T - 1) / a.E - c0 + 1;
+          if (rv::seq_whole(a, p, u)) {
+            CHECK(segments.count({k, u, -1}), "a whole unit left out");
+            continue;
+          }
+          const int c0 = rv::seq_chunk_at(a, rv::seq_pos(p, u, 0));
+          const int n = rv::seq_chunk_at(a, rv::seq_pos(p, u, T - 1)) - c0 + 1;
           parts = parts || shared || n > 1;
           for (int c = c0; c < c0 + n; ++c) {
             CHECK(segments.count({k, u, c}), "a segment left out");
