@@ -101,8 +101,8 @@ __device__ __forceinline__ void lds_load16_asm(const char* base, uint32_t off, u
   asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
 }
 
-// A tile's K and V into a ring stage by the whole workgroup: `st` is the LDS byte of the stage plus
-// this wave's row block (rows 8w .. 8w + 7; the second load of each fills rows 32 + 8w ..).
+// A tile's K and V into a ring stage by the whole workgroup: `st` is the LDS byte of the stage plus this wave's row
+// block (rows 8w .. 8w + 7; the second load of each fills rows 32 + 8w ..).
 __device__ __forceinline__ void load_tile(const TileRows& ts, uint32_t st) {
   const uint32_t r = threadIdx.x >> 3, c = threadIdx.x & 7;
   const uint32_t o0 = min(r, ts.last) * ts.row + 16u * (c ^ sw(r));
@@ -113,67 +113,64 @@ __device__ __forceinline__ void load_tile(const TileRows& ts, uint32_t st) {
   lds_load16_asm(ts.v, o1, st + TILE * 2 + 32 * D * 2);
 }
 
-// ---- 32 queries over NB blocks of 32 keys -----------------------------------------------------
+constexpr int kHalf = 32;  // keys of a wave's stage
 
-// Scores: entry r of s[i] is key 32 i + 8 (r / 4) + 4 half + r % 4.
-template <int NB>
-struct Scores {
-  f32x16 s[NB];
-};
-template <int NB>
-__device__ __forceinline__ void read_keys(const uint16_t* keys, int lane, bf16x8 (&kf)[NB][4]) {
+// ---- 32 queries over 32 keys ------------------------------------------------------------------
+
+// Scores: entry r is key 8 (r / 4) + 4 half + r % 4.
+__device__ __forceinline__ f32x16 score(const uint16_t* keys, const bf16x8 (&qf)[4], int lane) {
+  f32x16 z = {};
 #pragma unroll
   for (int ds = 0; ds < 4; ++ds)
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-      kf[i][ds] = *reinterpret_cast<const bf16x8*>(&keys[swz(32 * i + (lane & 31), ds * 2 + (lane >> 5))]);
-}
-template <int NB>
-__device__ __forceinline__ void score(const bf16x8 (&kf)[NB][4], const bf16x8 (&qf)[4], Scores<NB>& z) {
-#pragma unroll
-  for (int i = 0; i < NB; ++i) z.s[i] = f32x16{};
-#pragma unroll
-  for (int ds = 0; ds < 4; ++ds)
-#pragma unroll
-    for (int i = 0; i < NB; ++i) z.s[i] = mfma32(kf[i][ds], qf[ds], z.s[i]);
+    z = mfma32(*reinterpret_cast<const bf16x8*>(&keys[swz(lane & 31, ds * 2 + (lane >> 5))]), qf[ds], z);
+  return z;
 }
 // Keys >= valid get -1e30 (arithmetically: lane masks would take the scalar registers).
-template <int NB>
-__device__ __forceinline__ void mask_scores(Scores<NB>& z, int lane, int valid) {
+__device__ __forceinline__ void mask_scores(f32x16& z, int lane, int valid) {
   const float fv = (float)(valid - 4 * (lane >> 5) - 1);
 #pragma unroll
-  for (int i = 0; i < NB; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      z.s[i][r] = fmaf(__saturatef((float)(32 * i + 8 * (r >> 2) + (r & 3)) - fv), kNegBig, z.s[i][r]);
+  for (int r = 0; r < 16; ++r) z[r] = fmaf(__saturatef((float)(8 * (r >> 2) + (r & 3)) - fv), kNegBig, z[r]);
 }
 // p = 2^(z log2(e) / 8 - m), rounded to bf16 as the value product's operand; returns this lane's share of their
 // sum, of the unrounded ones (summed after rounding, two to an instruction, the log-sum-exp of 63 keys was 2e-4 off).
-template <int NB>
-__device__ __forceinline__ float exponentials(const Scores<NB>& z, float m, bf16x8 (&p)[2 * NB]) {
+__device__ __forceinline__ float exponentials(const f32x16& z, float m, bf16x8 (&p)[2]) {
   float sum = -0.f;  // -0 + x == x: the first add folds away
 #pragma unroll
-  for (int i = 0; i < NB; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; r += 2) {
-      const float e0 = __builtin_amdgcn_exp2f(fmaf(z.s[i][r], kScaleLog2, -m));
-      const float e1 = __builtin_amdgcn_exp2f(fmaf(z.s[i][r + 1], kScaleLog2, -m));
-      sum += e0 + e1;
-      p[2 * i + (r >> 3)][r & 7] = (__bf16)e0;
-      p[2 * i + (r >> 3)][(r & 7) + 1] = (__bf16)e1;
-    }
+  for (int r = 0; r < 16; r += 2) {
+    const float e0 = __builtin_amdgcn_exp2f(fmaf(z[r], kScaleLog2, -m));
+    const float e1 = __builtin_amdgcn_exp2f(fmaf(z[r + 1], kScaleLog2, -m));
+    sum += e0 + e1;
+    p[r >> 3][r & 7] = (__bf16)e0;
+    p[r >> 3][(r & 7) + 1] = (__bf16)e1;
+  }
   return sum;
 }
-// The end of the keys' softmax, by tile_compute's rule: where some lane's sum reaches 2^64 (every p is infinite while
-// the reference is unset), the reference is raised to the keys' maximum and p formed again.
-template <int NB>
-__device__ __forceinline__ void settle(const Scores<NB>& z, SoftmaxState& sm, bf16x8 (&p)[2 * NB], float sum) {
+
+// 32 keys and values in LDS.  The running reference follows tile_compute's rule: where some lane's sum reaches 2^64
+// (every p is infinite while the reference is unset) it is raised to the keys' maximum and p formed again.
+__device__ __forceinline__ void compute(const uint16_t* keys, const uint16_t* values, const bf16x8 (&qf)[4], int lane,
+                                        int valid, SoftmaxState& sm) {
+  f32x16 z = score(keys, qf, lane);
+  if (__builtin_expect(valid < kHalf, 0)) mask_scores(z, lane, valid);
+  // V^T fragments through transposing reads, as in tile_compute
+  bf16x8 vf[2][2], p[2];
+  const int g = lane >> 4, i16 = lane & 15, rr = i16 >> 2, jj = i16 & 3, hh = g >> 1;
+  const int col = 16 * (g & 1) + 4 * jj;
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+    for (int db = 0; db < 2; ++db) {
+      const int row = ks * 16 + 4 * hh + rr, lcol = db * 32 + col;
+      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(values + swz(row, lcol >> 3) + (lcol & 7)));
+      const i16x4 hi =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(values + swz(row + 8, lcol >> 3) + (lcol & 7)));
+      vf[ks][db] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  float sum = exponentials(z, sm.m, p);
   if (__builtin_expect(__any(!(sum < kOverflowGuard)), 0)) {
-    float mx = z.s[0][0];
+    float mx = z[0];
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, z.s[i][r]);
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, z[r]);
     const float m_new = fmaxf(sm.m, half_max(mx) * kScaleLog2);
     const float alpha = __builtin_amdgcn_exp2f(sm.m - m_new);
     sm.l *= alpha;
@@ -183,78 +180,15 @@ __device__ __forceinline__ void settle(const Scores<NB>& z, SoftmaxState& sm, bf
     sum = exponentials(z, m_new, p);
   }
   sm.l += sum;
-}
-// V^T fragments through transposing reads, as in tile_compute.
-template <int NB>
-__device__ __forceinline__ void read_values(const uint16_t* values, int lane, bf16x8 (&vf)[2 * NB][2]) {
-  const int g = lane >> 4, i16 = lane & 15, rr = i16 >> 2, jj = i16 & 3, hh = g >> 1;
-  const int col = 16 * (g & 1) + 4 * jj;
 #pragma unroll
-  for (int ks = 0; ks < 2 * NB; ++ks)
-#pragma unroll
-    for (int db = 0; db < 2; ++db) {
-      const int row = ks * 16 + 4 * hh + rr, lcol = db * 32 + col;
-      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(values + swz(row, lcol >> 3) + (lcol & 7)));
-      const i16x4 hi =
-          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(values + swz(row + 8, lcol >> 3) + (lcol & 7)));
-      vf[ks][db] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    }
-}
-template <int NB>
-__device__ __forceinline__ void add_values(const bf16x8 (&vf)[2 * NB][2], const bf16x8 (&p)[2 * NB], SoftmaxState& sm) {
-#pragma unroll
-  for (int ks = 0; ks < 2 * NB; ++ks) {
+  for (int ks = 0; ks < 2; ++ks) {
     sm.o0 = mfma32(vf[ks][0], p[ks], sm.o0);
     sm.o1 = mfma32(vf[ks][1], p[ks], sm.o1);
   }
 }
 
-// Keys and values in LDS, all of them at once.
-template <int NB>
-__device__ __forceinline__ void compute(const uint16_t* keys, const uint16_t* values, const bf16x8 (&qf)[4], int lane,
-                                        int valid, SoftmaxState& sm) {
-  Scores<NB> z;
-  bf16x8 kf[NB][4], vf[2 * NB][2], p[2 * NB];
-  read_keys<NB>(keys, lane, kf);
-  score(kf, qf, z);
-  if (__builtin_expect(valid < 32 * NB, 0)) mask_scores(z, lane, valid);
-  read_values<NB>(values, lane, vf);
-  settle(z, sm, p, exponentials(z, sm.m, p));
-  add_values<NB>(vf, p, sm);
-}
-
-// Two tiles: the scores of b are formed under the exponentials of a, and the value product of a under the
-// exponentials of b.  (Against one tile after the other: 4 to 5 % less where keys come from memory, 240 queries over
-// 52,000 rows, and the same within 1 % where they are in L2: there the two waves of a SIMD share its units to
-// the same effect whatever the order within a wave.)
-__device__ __forceinline__ void compute_pair(const uint16_t* a, const uint16_t* b, const bf16x8 (&qf)[4], int lane,
-                                             int valid_a, int valid_b, SoftmaxState& sm) {
-  Scores<2> za, zb;
-  bf16x8 kf[2][4], vf[4][2], pa[4], pb[4];
-  read_keys<2>(a, lane, kf);
-  score(kf, qf, za);
-  if (__builtin_expect(valid_a < BK, 0)) mask_scores(za, lane, valid_a);
-  __builtin_amdgcn_sched_barrier(0);
-  read_keys<2>(b, lane, kf);
-  read_values<2>(a + TILE, lane, vf);
-  __builtin_amdgcn_sched_barrier(0);
-  score(kf, qf, zb);
-  const float sum_a = exponentials(za, sm.m, pa);
-  __builtin_amdgcn_sched_barrier(0);
-  settle(za, sm, pa, sum_a);
-  if (__builtin_expect(valid_b < BK, 0)) mask_scores(zb, lane, valid_b);
-  __builtin_amdgcn_sched_barrier(0);
-  add_values<2>(vf, pa, sm);
-  const float sum_b = exponentials(zb, sm.m, pb);
-  __builtin_amdgcn_sched_barrier(0);
-  read_values<2>(b + TILE, lane, vf);
-  settle(zb, sm, pb, sum_b);
-  add_values<2>(vf, pb, sm);
-}
-
 // ---- few queries: every wave takes tiles of its own -------------------------------------------
 
-constexpr int kHalf = 32;                   // keys of a wave's stage
 constexpr int kHalfStage = 2 * kHalf * D;   // K rows then V rows: 8 KB
 constexpr int kHalfLoads = 8;               // load instructions of a stage
 static_assert(2 * 4 * kHalfStage == NSTAGE * STAGE, "four waves' two stages fill the same LDS");
@@ -368,7 +302,7 @@ __device__ __forceinline__ void narrow_segment(const SeqArgs& a, const SeqPass& 
     const bool more = i + 1 < n;
     if (more) next = order.rows(tc, i + 1);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kHalfLoads) : "memory");
-    compute<1>(st0, st0 + kHalf * D, qf, lane, valid, sm);
+    compute(st0, st0 + kHalf * D, qf, lane, valid, sm);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) {
       load_half(next, 0, ring, lane);
@@ -376,7 +310,7 @@ __device__ __forceinline__ void narrow_segment(const SeqArgs& a, const SeqPass& 
     } else {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
-    if (valid > kHalf) compute<1>(st1, st1 + kHalf * D, qf, lane, valid - kHalf, sm);
+    if (valid > kHalf) compute(st1, st1 + kHalf * D, qf, lane, valid - kHalf, sm);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) load_half(next, 1, ring + kHalfStage * 2, lane);
   }
@@ -432,21 +366,22 @@ __device__ __forceinline__ void wide_segment(const SeqArgs& a, const SeqPass& p,
   // (the queries pass through the wait: the compiler's own for them would wait for tiles in the loop)
   asm volatile("s_waitcnt vmcnt(0)" : "+v"(qf[0]), "+v"(qf[1]), "+v"(qf[2]), "+v"(qf[3])::"memory");
   __syncthreads();
-  auto step = [&](auto phase, int i) {
+  auto step = [&](auto phase, auto first, int i) {
     constexpr int P = decltype(phase)::value;
     if (i + 2 < n) load_tile(order.rows(tc, i + 2), ring + (P + 2) % NSTAGE * kStageBytes);
     if (i + 3 < n) load_tile(order.rows(tc, i + 3), ring + (P + 3) % NSTAGE * kStageBytes);
-    if (active && i + 1 < n)
-      compute_pair(lds + P * STAGE, lds + (P + 1) * STAGE, qf, lane, tc.valid(order.at(i)), tc.valid(order.at(i + 1)), sm);
-    else if (active)
-      compute<2>(lds + P * STAGE, lds + P * STAGE + TILE, qf, lane, tc.valid(order.at(i)), sm);
+    if (active) {
+      tile_compute<decltype(first)::value>(lds + P * STAGE, qf, lane, tc.valid(order.at(i)), sm);
+      if (i + 1 < n) tile_compute<false>(lds + (P + 1) * STAGE, qf, lane, tc.valid(order.at(i + 1)), sm);
+    }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
-  for (int i = 0; i < n; i = uniform(i + 4)) {
-    step(StageConst<0>{}, i);
+  step(StageConst<0>{}, std::true_type{}, 0);
+  for (int i = 2; i < n; i = uniform(i + 4)) {
+    step(StageConst<2>{}, std::false_type{}, i);
     if (i + 2 >= n) break;
-    step(StageConst<2>{}, i + 2);
+    step(StageConst<0>{}, std::false_type{}, i + 2);
   }
 
   // Rows through LDS, so that whole rows are written (the ring is free: the last step ended in a barrier).
@@ -461,15 +396,25 @@ __device__ __forceinline__ void wide_segment(const SeqArgs& a, const SeqPass& p,
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    float* const slot = g.slots ? g.slots + wave * kSubFloats : nullptr;
+    if (g.slots) {
+      // all 32 rows (those past the last query's are never read), 1 KB of them a store
+      float* const slot = g.slots + wave * kSubFloats;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int rr = 8 * i + (lane >> 3), d8 = (lane & 7) * 8;
-      if (q0 + rr >= rows) continue;
-      float o[8];
+      for (int i = 0; i < 8; ++i) {
+        const int rr = 4 * i + (lane >> 4), d4 = (lane & 15) * 4;
+        *reinterpret_cast<float4*>(slot + rr * D + d4) = *reinterpret_cast<const float4*>(st + rr * kRowStride + d4);
+      }
+      slot[kSubRows * D + lane] = half ? s_l[wave][l32] : s_m[wave][l32];
+    } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = st[rr * kRowStride + d8 + e];
-      write_row(a, p, g.h, q0 + rr, d8, o, s_m[wave][rr], s_l[wave][rr], slot);
+      for (int i = 0; i < 4; ++i) {
+        const int rr = 8 * i + (lane >> 3), d8 = (lane & 7) * 8;
+        if (q0 + rr >= rows) continue;
+        float o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = st[rr * kRowStride + d8 + e];
+        write_row(a, p, g.h, q0 + rr, d8, o, s_m[wave][rr], s_l[wave][rr], nullptr);
+      }
     }
   }
   __syncthreads();  // (the LDS is the next segment's)
@@ -478,16 +423,51 @@ __device__ __forceinline__ void wide_segment(const SeqArgs& a, const SeqPass& p,
 __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
   __shared__ __attribute__((aligned(16))) uint16_t lds[NSTAGE * STAGE];
   __shared__ float s_m[4][kSubRows], s_l[4][kSubRows];
-  const int c = uniform(seq_chunk_of(a, (int)blockIdx.x));
+  const int c = uniform(seq_chunk_of(a, (int)blockIdx.x, (int)blockIdx.y));
   if (c < 0) return;
   const int H = a.n_heads;
-  int done = 0;  // tiles this workgroup has taken
-  auto run = [&](int ip, int unit, int T, int t0, int t1, float* slots) {
-    const SeqPass& p = a.pass[ip];
+  // A whole unit of each round, then the chunk's segments.
+  const int begin = a.pos_first + c * a.E, end = c < a.chunks ? min(begin + a.E, a.total) : 0;
+  int round = c < a.width ? 0 : a.rounds;
+  int pos = begin;  // the chunk's positions from here on are still to be done
+  int ip = round < a.rounds ? 0 : last_at_or_below(0, a.n_pass, begin, [&](int i) { return a.pos0[i]; });
+  int done = 0;     // tiles this workgroup has taken of its chunk
+  while (round < a.rounds || pos < end) {
+    const bool whole = round < a.rounds;
+    int unit;
     Segment g;
-    g.t0 = t0;
-    g.t1 = t1;
-    g.slots = slots;
+    if (whole) {
+      const int u = uniform(round * a.width + c);
+      ip = last_at_or_below(0, a.n_pass, u, [&](int i) { return a.unit0[i]; });
+      unit = u - a.unit0[ip];
+      g.t0 = 0;
+      g.t1 = seq_tiles(a.pass[ip]);
+      g.slots = nullptr;
+    } else {
+      const SeqPass& p = a.pass[ip];
+      const int T = seq_tiles(p), units = H * p.q_tiles;
+      unit = 0;
+      const int t0 = T == 0 ? 0 : uniform(seq_first_tile(p, T, pos - p.pos0, &unit));
+      unit = uniform(unit);
+      if (T == 0 || unit >= units) {
+        if (++ip >= a.n_pass) break;
+        pos = max(pos, a.pos0[ip]);  // (the chunk may begin inside the last tile before it)
+        continue;
+      }
+      int end_unit = 0;
+      const int end_tile = uniform(seq_first_tile(p, T, end - p.pos0, &end_unit));
+      const int t1 = uniform(end_unit) > unit ? T : end_tile;
+      if (uniform(end_unit) < unit || t1 <= t0) break;  // the last positions belong to a tile that began before
+      const bool shared = ip < a.n_inner || p.parent >= 0;
+      g.t0 = t0;
+      g.t1 = t1;
+      g.slots = !shared && t0 == 0 && t1 == T
+                    ? nullptr
+                    : a.part + (int64_t)seq_slot(p, shared, unit, c, uniform(seq_chunk_at(a, seq_pos(p, unit, 0)))) *
+                                   kSubFloats;
+    }
+    const SeqPass& p = a.pass[ip];
+    const int T = seq_tiles(p);
     // query tiles of a head are neighbours
     g.h = uniform(unit / p.q_tiles);
     g.qt = unit - g.h * p.q_tiles;
@@ -510,45 +490,17 @@ __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
       // same few tiles at a time and find them in their XCD's L2.  (In key order each fetched its keys from beyond
       // it, and that was the bound: 1041 queries over 52,000 rows 342 -> 322 us.)
       const int per = uniform(max(1, a.E / p.cost));
-      const int ahead = uniform((done - t0) % per);
-      g.ts = t0 + (ahead < 0 ? ahead + per : ahead);
-      if (g.ts >= t1) g.ts = t0;
+      const int ahead = uniform((done - g.t0) % per);
+      g.ts = g.t0 + (ahead < 0 ? ahead + per : ahead);
+      if (whole || g.ts >= g.t1) g.ts = g.t0;
       wide_segment(a, p, tc, g, lds, s_m, s_l);
     }
-    done += t1 - t0;
-  };
-  for (int r = 0; r < a.rounds && c < a.width; ++r) {
-    const int u = uniform(r * a.width + c);
-    const int ip = last_at_or_below(0, a.n_pass, u, [&](int i) { return a.unit0[i]; });
-    const int T = seq_tiles(a.pass[ip]);
-    run(ip, u - a.unit0[ip], T, 0, T, nullptr);
-  }
-  if (c >= a.chunks) return;
-  const int begin = a.pos_first + c * a.E, end = min(begin + a.E, a.total);
-  done = 0;
-  int ip = last_at_or_below(0, a.n_pass, begin, [&](int i) { return a.pos0[i]; });
-  for (int pos = begin; pos < end;) {  // pos: the chunk's positions from here on are still to be done
-    const SeqPass& p = a.pass[ip];
-    const int T = seq_tiles(p), units = H * p.q_tiles;
-    int unit = 0;
-    const int t0 = T == 0 ? 0 : uniform(seq_first_tile(p, T, pos - p.pos0, &unit));
-    unit = uniform(unit);
-    if (T == 0 || unit >= units) {
-      if (++ip >= a.n_pass) break;
-      pos = max(pos, a.pos0[ip]);  // (the chunk may begin inside the last tile before it)
-      continue;
+    if (whole) {
+      if (++round == a.rounds && pos < end) ip = last_at_or_below(0, a.n_pass, begin, [&](int i) { return a.pos0[i]; });
+    } else {
+      done += g.t1 - g.t0;
+      pos = g.t1 < T ? end : seq_pos(p, unit + 1, 0);
     }
-    int end_unit = 0;
-    const int end_tile = uniform(seq_first_tile(p, T, end - p.pos0, &end_unit));
-    const int t1 = uniform(end_unit) > unit ? T : end_tile;
-    if (uniform(end_unit) < unit || t1 <= t0) break;  // the last positions belong to a tile that began before
-    const bool shared = ip < a.n_inner || p.parent >= 0;
-    float* const slots = !shared && t0 == 0 && t1 == T
-                             ? nullptr
-                             : a.part + (int64_t)seq_slot(p, shared, unit, c, uniform(seq_chunk_at(a, seq_pos(p, unit, 0)))) *
-                                            kSubFloats;
-    run(ip, unit, T, t0, t1, slots);
-    pos = t1 < T ? end : seq_pos(p, unit + 1, 0);
   }
 }
 
@@ -560,7 +512,7 @@ __device__ __forceinline__ void merge_rows(const SeqArgs& a, const SeqPass& leaf
   const int G = a.group, lane = threadIdx.x & 63;
   const int grp = kOne ? lane >> 4 : 0, d4 = (lane & 15) * 4;
   constexpr int kStep = kOne ? 4 : 1;
-  constexpr int kBatch = kOne ? 4 : 2;  // segments a lane has in flight together
+  constexpr int kBatch = 4;             // segments a lane has in flight together
   constexpr int kLevels = 3;            // passes whose segments are taken as one list
   float mmax = kNegBig, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -664,7 +616,7 @@ __global__ __launch_bounds__(256) void seq_merge_kernel(SeqArgs a) {
 
 hipError_t launch_attend_seqs(const SeqArgs& a, hipStream_t s) {
   if (seq_grid(a) > 0) {
-    hipLaunchKernelGGL(seq_fwd_kernel, dim3((unsigned)seq_grid(a)), dim3(kAttnThreads), 0, s, a);
+    hipLaunchKernelGGL(seq_fwd_kernel, dim3((unsigned)a.n_queues, (unsigned)seq_grid(a)), dim3(kAttnThreads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -224,6 +224,9 @@ constexpr int kSubRows = 32;  // rows of a partial slot of this launch
 constexpr int kSubFloats = kSubRows * kHeadDim + 2 * kSubRows;  // fp32 rows, references, row sums
 constexpr int kSubsPerTile = kAttnBQ / kSubRows;
 constexpr int kMergeOne = 4, kMergeFew = 16;  // rows a merge workgroup takes: a wave one, or four
+struct SeqShares {
+  int32_t each, more;  // chunks an XCD, and XCDs that take one more
+};
 struct SeqArgs {
   const uint16_t *Q, *K, *V;      // packed frames [tokens][Hq or H][64]; K, V NULL without frame keys
   const uint16_t *pageK, *pageV;  // [H][n_pages][64][64]
@@ -236,6 +239,7 @@ struct SeqArgs {
   int rounds, width;              // whole units to a workgroup, and workgroups that take them
   int pos_first, total, E, chunks;  // positions of the units that are cut: [pos_first, total), chunks of E
   int inner_chunks;               // chunks that begin in an inner pass
+  SeqShares inner, leaves;        // the XCDs' shares of them and of the others (and places in a round)
   int n_queues;                   // XCDs that the workgroups are dealt over
   int merge_blocks;
   int32_t pos0[kMaxPasses];    // the passes' first positions and units, again (a workgroup finds its pass by them)
@@ -257,25 +261,19 @@ RV_HD inline int seq_first_tile(const SeqPass& p, int T, int off, int* unit) {
   *unit = t < T ? u : u + 1;
   return t < T ? t : 0;
 }
-// The chunk (and place in a round) of a workgroup, or -1.  Workgroups are dealt to the XCDs in turn; consecutive chunks (query
-// tiles of a head) go to one XCD, and each XCD gets its share of the inner passes' chunks, which are
-// bound by arithmetic, and of the leaves', which are bound by memory.
-RV_HD inline int seq_share(int n, int x, int X) { return (int)((int64_t)n * x / X); }
+// The chunk (and place in a round) of workgroup (x, j), or -1.  Workgroups are dealt to the XCDs in turn, x first;
+// consecutive chunks (query tiles of a head) go to one XCD, and each XCD gets its share of the inner passes' chunks,
+// which are bound by arithmetic, and of the leaves', which are bound by memory.
+RV_HD inline int seq_share0(const SeqShares& s, int x) { return x * s.each + (x < s.more ? x : s.more); }
 template <class A>
-RV_HD inline int seq_chunk_of(const A& a, int block) {
-  const int X = a.n_queues, x = block % X, all = a.rounds > 0 && a.width > a.chunks ? a.width : a.chunks;
-  const int rest = all - a.inner_chunks;
-  int j = block / X;
-  const int i0 = seq_share(a.inner_chunks, x, X), ni = seq_share(a.inner_chunks, x + 1, X) - i0;
-  if (j < ni) return i0 + j;
-  j -= ni;
-  const int l0 = seq_share(rest, x, X), nl = seq_share(rest, x + 1, X) - l0;
-  return j < nl ? a.inner_chunks + l0 + j : -1;
+RV_HD inline int seq_chunk_of(const A& a, int x, int j) {
+  const int ni = a.inner.each + (x < a.inner.more ? 1 : 0), nl = a.leaves.each + (x < a.leaves.more ? 1 : 0);
+  if (j < ni) return seq_share0(a.inner, x) + j;
+  return j - ni < nl ? a.inner_chunks + seq_share0(a.leaves, x) + j - ni : -1;
 }
 template <class A>
-RV_HD inline int seq_grid(const A& a) {
-  const int X = a.n_queues, all = a.rounds > 0 && a.width > a.chunks ? a.width : a.chunks;
-  return X * ((a.inner_chunks + X - 1) / X + (all - a.inner_chunks + X - 1) / X);
+RV_HD inline int seq_grid(const A& a) {  // workgroups an XCD
+  return a.inner.each + (a.inner.more > 0) + a.leaves.each + (a.leaves.more > 0);
 }
 
 template <class A>

@@ -189,8 +189,21 @@ constexpr int kWideCost = 4, kWideFixed = 16, kNarrowCost = 2, kNarrowFixed = 16
 constexpr int kMinChunk = 20;     // positions
 // (no chunk between a unit's first and last is without a tile of it)
 static_assert(kMinChunk >= kWideFixed + kWideCost && kMinChunk >= kNarrowFixed + kNarrowCost, "chunk length");
+// Where all units have one length, they are cut into equal pieces, so that the query tiles of a head go over the same
+// keys, unless chunks that run from one unit into the next are shorter by more than this many tiles; and left whole
+// where pieces would be shorter by no more than this.  (1041 queries of 16 heads: over 2000, 5000 and 10,000 rows 3
+// pieces 36, 49 and 78 us, running chunks 40, 55 and 82; 20,000 rows the same; 52,000 rows 319 and 301.  Over 64 rows whole
+// units 22.7 us, 3 pieces 25.8; over 1000 rows 35 and 31.)
+constexpr int kStartTiles = 16;
 constexpr int kPartialTiles = 5;  // key tiles that a unit's partial result takes as long as
 constexpr int kFewSegments = 4;   // up to which the merge takes a row in 16 lanes
+
+// First position of unit u of all passes' units.
+int first_pos(const SeqArgs& a, int u) {
+  int i = a.n_pass - 1;
+  while (i > 0 && a.unit0[i] > u) --i;
+  return seq_pos(a.pass[i], u - a.unit0[i], 0);
+}
 
 struct Builder {
   const PageBook& book;
@@ -313,37 +326,44 @@ int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool 
     // The device's workgroup slots.  (With inner passes an XCD's two shares are rounded up each: a workgroup more
     // than its slots would wait for a whole chunk.)
     const int at_once = std::max(1, kAttnWgPerCu * n_cus - (a->n_inner > 0 ? a->n_queues : 0));
-    a->total = (int)pos;
-    a->pos_first = 0;
     a->rounds = alike ? (int)(units / at_once) : 0;
     a->width = at_once;
-    if (a->rounds > 0) {
-      const int first = a->rounds * at_once;  // the first unit that is cut
-      int i = a->n_pass - 1;
-      while (i > 0 && a->unit0[i] > first) --i;
-      a->pos_first = first < units ? seq_pos(a->pass[i], first - a->unit0[i], 0) : a->total;
-      units -= first;
+    a->total = (int)pos;
+    const int first = a->rounds * at_once;  // the first unit that is cut
+    a->pos_first = first == 0 ? 0 : first < units ? first_pos(*a, first) : a->total;
+    a->E = (int)std::max<int64_t>(kMinChunk, ceil_div64(a->total - a->pos_first, at_once));
+    if (alike && longest == shortest && first < units) {
+      // units of one length in equal pieces: a tile takes `pieces` positions and a chunk as many as a unit has tiles
+      const int64_t T = seq_tiles(a->pass[0]), even = ceil_div64((units - first) * T, at_once);
+      int64_t pieces = std::min<int64_t>(at_once / (units - first), std::max<int64_t>(1, T * kWideCost / kMinChunk));
+      if (T - ceil_div64(T, pieces) <= kStartTiles) pieces = 1;
+      if (units * T * pieces <= INT32_MAX / 2 && ceil_div64(T, pieces) <= even + kStartTiles) {
+        for (int i = 0; i < a->n_pass; ++i) {
+          SeqPass& p = a->pass[i];
+          p.cost = (int)pieces;
+          p.fixed = 0;
+          a->pos0[i] = p.pos0 = (int)(p.unit0 * T * pieces);
+        }
+        a->total = (int)(units * T * pieces);
+        a->pos_first = (int)(first * T * pieces);
+        a->E = (int)T;
+      }
     }
-    // Chunks of equal length, one for each slot, but no shorter than kMinChunk.  Units of one length are cut into equal
-    // pieces instead where that takes no longer than a second unit's start would.
-    const int64_t rest = a->total - a->pos_first;
-    a->E = (int)std::max<int64_t>(kMinChunk, ceil_div64(rest, at_once));
-    if (alike && longest == shortest && units > 0 && units <= at_once) {
-      const int64_t piece = ceil_div64(longest, at_once / units);
-      if (piece >= kMinChunk && piece <= a->E + kWideFixed) a->E = (int)ceil_div64(longest, ceil_div64(longest, piece));
-    }
-    a->chunks = (int)ceil_div64(rest, a->E);
+    a->chunks = (int)ceil_div64(a->total - a->pos_first, a->E);
     const int leaf0 = a->n_inner < a->n_pass ? a->pass[a->n_inner].pos0 : a->total;
     a->inner_chunks = (int)ceil_div64(leaf0, a->E);
+    const int X = a->n_queues, rest = (a->rounds > 0 ? std::max(a->width, a->chunks) : a->chunks) - a->inner_chunks;
+    a->inner = {a->inner_chunks / X, a->inner_chunks % X};
+    a->leaves = {rest / X, rest % X};
     int64_t slots = (2 * (int64_t)a->chunks + 1) * kSubsPerTile, merge = 0;
     for (int i = 0; i < a->n_pass; ++i) {
       SeqPass& p = a->pass[i];
       const int n_units = p.q_tiles * n_heads, T = seq_tiles(p);
       const bool leaf = i >= a->n_inner, shared = !leaf || p.parent >= 0;
       if (shared && T > 0) {
-        const int first = seq_chunk_at(*a, p.pos0), last = seq_chunk_at(*a, seq_pos(p, n_units - 1, T - 1));
-        p.slot0 = (int)(slots - (int64_t)first * (p.tile_rows / kSubRows));
-        slots += (int64_t)(n_units + last - first) * (p.tile_rows / kSubRows);
+        const int c0 = seq_chunk_at(*a, p.pos0), c1 = seq_chunk_at(*a, seq_pos(p, n_units - 1, T - 1));
+        p.slot0 = (int)(slots - (int64_t)c0 * (p.tile_rows / kSubRows));
+        slots += (int64_t)(n_units + c1 - c0) * (p.tile_rows / kSubRows);
         fits = fits && slots <= max_slots;
       }
       a->merge0[i] = (int)merge;

@@ -168,8 +168,9 @@ struct World {
         return i;
       };
       std::vector<int> order;
-      for (int b = 0; b < rv::seq_grid(a); ++b)
-        if (rv::seq_chunk_of(a, b) >= 0) order.push_back(rv::seq_chunk_of(a, b));
+      for (int j = 0; j < rv::seq_grid(a); ++j)
+        for (int x = 0; x < a.n_queues; ++x)
+          if (rv::seq_chunk_of(a, x, j) >= 0) order.push_back(rv::seq_chunk_of(a, x, j));
       std::vector<int> sorted = order;
       std::sort(sorted.begin(), sorted.end());
       const int places = a.rounds > 0 ? std::max(a.width, a.chunks) : a.chunks;
