@@ -16,13 +16,12 @@
 namespace rv {
 namespace {
 
-// The last i in [i0, n) whose value is at or below x (they ascend).
-template <class F>
-__device__ __forceinline__ int last_at_or_below(int i0, int n, int x, F value) {
-  const int lane = threadIdx.x & 63;
-  int count = 0;
-  for (int i = i0; i < n; i += 64) count += __popcll(__ballot(i + lane < n && value(min(i + lane, n - 1)) <= x));
-  return uniform(i0 + count - 1);
+// The last i in [i0, n) with values[i] <= x (they ascend, and the first is not above x).  The load waits for no
+// other one: every lane's element is there, whatever i0 and n.
+static_assert(kMaxPasses <= 64, "a lane each");
+__device__ __forceinline__ int last_at_or_below(const int32_t (&values)[kMaxPasses], int i0, int n, int x) {
+  const int lane = threadIdx.x & 63, v = values[min(lane, kMaxPasses - 1)];
+  return uniform(63 - __builtin_clzll(__ballot(lane >= i0 && lane < n && v <= x) | 1));
 }
 
 // The key tiles of a workgroup's pass: pages, then frame rows.
@@ -430,7 +429,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
   const int begin = a.pos_first + c * a.E, end = c < a.chunks ? min(begin + a.E, a.total) : 0;
   int round = c < a.width ? 0 : a.rounds;
   int pos = begin;  // the chunk's positions from here on are still to be done
-  int ip = round < a.rounds ? 0 : last_at_or_below(0, a.n_pass, begin, [&](int i) { return a.pos0[i]; });
+  int ip = round < a.rounds ? 0 : last_at_or_below(a.pos0, 0, a.n_pass, begin);
   int done = 0;     // tiles this workgroup has taken of its chunk
   while (round < a.rounds || pos < end) {
     const bool whole = round < a.rounds;
@@ -438,7 +437,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
     Segment g;
     if (whole) {
       const int u = uniform(round * a.width + c);
-      ip = last_at_or_below(0, a.n_pass, u, [&](int i) { return a.unit0[i]; });
+      ip = last_at_or_below(a.unit0, 0, a.n_pass, u);
       unit = u - a.unit0[ip];
       g.t0 = 0;
       g.t1 = seq_tiles(a.pass[ip]);
@@ -496,7 +495,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
       wide_segment(a, p, tc, g, lds, s_m, s_l);
     }
     if (whole) {
-      if (++round == a.rounds && pos < end) ip = last_at_or_below(0, a.n_pass, begin, [&](int i) { return a.pos0[i]; });
+      if (++round == a.rounds && pos < end) ip = last_at_or_below(a.pos0, 0, a.n_pass, begin);
     } else {
       done += g.t1 - g.t0;
       pos = g.t1 < T ? end : seq_pos(p, unit + 1, 0);
@@ -600,7 +599,7 @@ __device__ __forceinline__ void merge_rows(const SeqArgs& a, const SeqPass& leaf
 
 __global__ __launch_bounds__(256) void seq_merge_kernel(SeqArgs a) {
   const int H = a.n_heads, wave = threadIdx.x >> 6;
-  const int ip = last_at_or_below(a.n_inner, a.n_pass, (int)blockIdx.x, [&](int i) { return a.merge0[i]; });
+  const int ip = last_at_or_below(a.merge0, a.n_inner, a.n_pass, (int)blockIdx.x);
   const SeqPass& leaf = a.pass[ip];
   const int b = (int)blockIdx.x - a.merge0[ip];
   const int h = uniform(b % H), row0 = uniform(b / H * leaf.merge_rows), rows = leaf.n_tok * a.group;
