@@ -8,6 +8,14 @@
 // each.  Softmax sums of disjoint key sets combine exactly, so a segment of a unit writes its
 // sums with their reference, and the merge launch joins, per query, the segments of its sequence's
 // pass and of the passes above it, in a fixed order.
+//
+// A query tile has 128 rows, 32 a wave, over key tiles that the workgroup loads together (as attend.hip's core), or
+// 32 where a pass has no more, each wave taking key tiles of its own and no barrier among them.  What bounds them:
+// many queries, the core's stalls (attend.hip): four sequences' frames of 1041 tokens over 5000 shared rows and 100 to
+// 430 of their own 152 us, 710 TFLOP/s; one frame over 52,000 rows 290 us.  Few queries over long rows, memory: 48
+// sequences of 5 tokens over 52,000 shared rows and 242 to 1041 of their own 106 us for 340 MB, 3.2 TB/s.  A token
+// each of 16 sequences, latency: 18 us, 13 of them the forward launch (3.6 until it has its place, 2 for the first
+// keys, the rest two or three tiles and the write of the sums), 5 the merge.
 #include <type_traits>
 
 #include "attn_tile.h"
@@ -506,6 +514,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
 // Joins the segments of a sequence's rows, 16 lanes a row's 64 elements.  Where a row has many segments
 // a wave takes one row and its four groups of lanes every fourth segment each (kOne); where it has few, each
 // group takes a row of its own.
+// (Bound by latency: a launch of 5 to 6 us, 1.4 of which an empty one takes; the sums are fp32, 14 MB of them for a
+// frame in three pieces.)
 template <bool kOne>
 __device__ __forceinline__ void merge_rows(const SeqArgs& a, const SeqPass& leaf, int ip, int h, int row) {
   const int G = a.group, lane = threadIdx.x & 63;

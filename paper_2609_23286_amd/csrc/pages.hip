@@ -1,12 +1,12 @@
 // pages.hip -- rows into, out of and within the pages of a pool, gfx950.
 //
 // A page is 64 rows of every head; its rows of head h are [64][64] bf16 at page number `page` of the head's own
-// array, for K and the same for V ([H][n_pages][64][64]: with all heads of a page together, a head's pages would lie
-// a power of two apart and share a sixteenth of the L2's sets).  A sequence's pages are listed in its row of the
-// device's page table.  All kernels here move 16-byte chunks, eight lanes to a
-// row's 128 bytes, so that every access is whole cache lines whatever rows are picked; they are
-// bound by memory, and read and write past the caches' reuse (nontemporal: halving two memories of 52,000 rows
-// and reading them back 184 -> 163 us, at 5.2 TB/s).  A workgroup finds its sequence by its first-block number.
+// array, for K and the same for V ([H][n_pages][64][64]: with all heads of a page together halving two memories of
+// 52,000 rows took 162 us instead of 152).  A sequence's pages are listed in its row of the device's page table.  All
+// kernels here move 16-byte chunks, eight lanes to a row's 128 bytes, so that every access is whole cache lines
+// whatever rows are picked; they are bound by memory, and read and write past the caches' reuse (nontemporal: 184
+// -> 162 us for the same).  Those 152 us move 852 MB (the kept rows to new pages and out again) at 5.6 TB/s, as much
+// as a large copy reaches.  A workgroup finds its sequence by its first-block number.
 #include "rv_internal.h"
 #include "rv_ops.h"
 

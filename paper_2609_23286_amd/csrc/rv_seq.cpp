@@ -180,23 +180,25 @@ int common_pages(const PageBook& book, int a, int b) {
   return i;
 }
 
-// Positions of a key tile and, once, of a unit: for a workgroup's 128 rows, and for 32 (where the waves
-// take tiles side by side), in about 0.35 us.  (Fixed shares of 8 to 24 and 6 to 20, tile costs of 1 to 4
-// for the narrow units and shortest chunks of 8 to 32 measured on twelve batches, from two single tokens to
-// 16 frames: these are within 4 % of the best of each but one, where narrow tiles of cost 1 and units of 20
-// are 5 % faster; without fixed shares long batches lost 10 to 40 %.)
+// Positions of a key tile and, once, of a unit: for a workgroup's 128 rows, and for 32 (where the waves take tiles
+// side by side).  (Fixed shares of 8 to 24 and 6 to 20, tile costs of 1 to 4 for the narrow units and shortest
+// chunks of 8 to 32 measured on twelve batches, from two single tokens to 16 frames: these were within 4 % of the
+// best of each but one, where narrow tiles of cost 1 and units of 20 were 5 % faster; without fixed shares long
+// batches lost 10 to 40 %.)
 constexpr int kWideCost = 4, kWideFixed = 16, kNarrowCost = 2, kNarrowFixed = 16;
 constexpr int kMinChunk = 20;     // positions
 // (no chunk between a unit's first and last is without a tile of it)
 static_assert(kMinChunk >= kWideFixed + kWideCost && kMinChunk >= kNarrowFixed + kNarrowCost, "chunk length");
-// Where all units have one length, they are cut into equal pieces, so that the query tiles of a head go over the same
-// keys, unless chunks that run from one unit into the next are shorter by more than this many tiles; and left whole
-// where pieces would be shorter by no more than this.  (1041 queries of 16 heads: over 2000, 5000 and 10,000 rows 3
-// pieces 36, 49 and 78 us, running chunks 40, 55 and 82; 20,000 rows the same; 52,000 rows 319 and 301.  Over 64 rows whole
-// units 22.7 us, 3 pieces 25.8; over 1000 rows 35 and 31.)
+// Where all units have one length, they are cut into equal pieces, so that the query tiles of a head go over the
+// same keys, unless chunks that run from one unit into the next are shorter by more than this many tiles; and
+// they are left whole where pieces would be shorter by no more than this.  (1041 queries of 16 heads: over 2000,
+// 5000 and 10,000 rows three pieces 36, 49 and 76 us, running chunks 44, 56 and 79; over 20,000 the same; over 52,000
+// 319 and 300.  Over 64 rows whole units 22.3 us, three pieces 24.6; over 1000 rows 35 and 31.)
 constexpr int kStartTiles = 16;
 constexpr int kPartialTiles = 5;  // key tiles that a unit's partial result takes as long as
-constexpr int kFewSegments = 4;   // up to which the merge takes a row in 16 lanes
+// Up to which the merge takes a row in 16 lanes, four segments at a time, and above it a wave a row, 16 at a time.
+// (1041 queries over 52,000 rows, five segments: 290 us with 16 lanes, 296 with a wave.)
+constexpr int kFewSegments = 6;
 
 // First position of unit u of all passes' units.
 int first_pos(const SeqArgs& a, int u) {

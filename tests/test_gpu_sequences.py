@@ -294,6 +294,23 @@ def test_whole_frames_over_a_shared_prefix(rv):
     w.check_attention([a], [1374], frame=True, scale=3.0)
 
 
+@pytest.mark.parametrize("H,lengths,tokens", [
+    (16, [130] * 8, 513),               # more query tiles than workgroups at a time: some are dealt out whole
+    (16, [130, 200, 129, 250] * 2, 513),  # and of different lengths
+    (16, [64] * 7, 640),                # 560 tiles: a round and a small rest
+    (2, [3000], 300),                   # six tiles, each in equal pieces
+    (2, [3000, 3000], 129),
+    (1, [40], 300),                     # short: whole tiles
+    (2, [5000, 2000], 300),             # different lengths: chunks that run from one tile into the next
+    (16, [1500], 1041),
+], ids=str)
+def test_strangers_with_many_queries(rv, H, lengths, tokens):
+    w = World(rv, H, sum(n // 64 + 2 for n in lengths), len(lengths), max(lengths) + 64)
+    seqs = [w.open() for _ in lengths]
+    w.append(seqs, lengths)
+    w.check_attention(seqs, [tokens] * len(seqs), frame=True)
+
+
 def test_more_sequences_than_a_launch_takes(rv):
     w = World(rv, 2, 700, 200, 600)
     a = w.open()
