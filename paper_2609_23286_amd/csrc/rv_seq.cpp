@@ -372,7 +372,9 @@ int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool 
       if (!leaf) continue;
       // merged: sums in parts, or none at all
       int most = T == 0 ? 2 : 1;
-      for (int u = 0; u < n_units && T > 0; ++u)
+      // chunks that a unit can lie in (in equal pieces: that each does)
+      const int64_t bound = T == 0 ? 0 : p.fixed == 0 ? p.cost : ceil_div64(seq_pos(p, 0, T - 1) - p.pos0, a->E) + 1;
+      for (int u = 0; u < n_units && most < bound; ++u)
         if (!seq_whole(*a, p, u))
           most = std::max(most, seq_chunk_at(*a, seq_pos(p, u, T - 1)) - seq_chunk_at(*a, seq_pos(p, u, 0)) + 1);
       p.merge_rows = shared || most > kFewSegments ? kMergeOne : kMergeFew;
