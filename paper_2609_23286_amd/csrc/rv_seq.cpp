@@ -197,8 +197,9 @@ static_assert(kMinChunk >= kWideFixed + kWideCost && kMinChunk >= kNarrowFixed +
 constexpr int kStartTiles = 16;
 constexpr int kPartialTiles = 5;  // key tiles that a unit's partial result takes as long as
 // Up to which the merge takes a row in 16 lanes, four segments at a time, and above it a wave a row, 16 at a time.
-// (1041 queries over 52,000 rows, five segments: 290 us with 16 lanes, 296 with a wave.)
-constexpr int kFewSegments = 6;
+// (1041 queries over 52,000 rows, five segments: 290 us with 16 lanes, 296 with a wave; four sequences' frames over
+// 5000 shared rows, nine segments: 150 and 154.)
+constexpr int kFewSegments = 12;
 
 // First position of unit u of all passes' units.
 int first_pos(const SeqArgs& a, int u) {
