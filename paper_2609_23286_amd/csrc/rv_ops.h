@@ -199,7 +199,7 @@ class PageBook {
 //
 // A unit is one query tile of one kv head of a pass; its work is the pass's key tiles, each of
 // `cost` positions, and `fixed` more before its second.  Units are numbered through all passes.  Where they are
-// alike and more than the device's workgroup slots, the first `rounds` times `width` are dealt out whole, one of a
+// more than the device's workgroup slots, the first `rounds` times `width` may be dealt out whole, one of a
 // round to each workgroup, so that neighbours (query tiles of a head) go over the same keys at the same time.
 // The positions of the others, one unit after another from pos_first on, are cut into chunks of E, one workgroup
 // each: a tile belongs to the chunk that its first position lies in.

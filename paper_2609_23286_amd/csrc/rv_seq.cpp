@@ -202,10 +202,30 @@ constexpr int kPartialTiles = 5;  // key tiles that a unit's partial result take
 constexpr int kFewSegments = 12;
 
 // First position of unit u of all passes' units.
-int first_pos(const SeqArgs& a, int u) {
+int first_pos(const SeqArgs& a, int64_t u) {
   int i = a.n_pass - 1;
   while (i > 0 && a.unit0[i] > u) --i;
-  return seq_pos(a.pass[i], u - a.unit0[i], 0);
+  return seq_pos(a.pass[i], (int)(u - a.unit0[i]), 0);
+}
+
+// Rounds of whole units, one to each of `width` workgroups: as many as the units fill, unless the one whose units are
+// the longest would work kWholeMore percent longer than with all units cut into equal chunks.  (16 frames of 1041
+// tokens over 5100 to 6000 rows of their own: whole units 598 us, chunks 733; over 750 to 6000 rows 413 and 466.  4
+// frames, a round of 3.5 of them: over 4200 to 6000 rows, 10 % longer, 154 and 159; 3000 to 6000, 19 %, 149 and 148; 600
+// to 6000, 40 %, 145 and 115.)
+constexpr int kWholeMore = 15;
+int whole_rounds(const SeqArgs& a, int64_t units, int64_t total, int width) {
+  const int rounds = (int)(units / width);
+  if (rounds == 0) return 0;
+  const int64_t cut = (int64_t)rounds * width, rest = cut < units ? total - first_pos(a, cut) : 0;
+  int64_t most = 0;  // of a workgroup's whole units; workgroups between two places where a pass begins have the same
+  for (int i = 0; i < a.n_pass; ++i) {
+    int64_t sum = 0;
+    for (int64_t u = a.unit0[i] % width; u < cut; u += width)
+      sum += (u + 1 < units ? first_pos(a, u + 1) : total) - first_pos(a, u);
+    most = std::max(most, sum);
+  }
+  return (most + ceil_div64(rest, width)) * 100 <= ceil_div64(total, width) * (100 + kWholeMore) ? rounds : 0;
 }
 
 struct Builder {
@@ -305,7 +325,7 @@ int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool 
     std::copy(b.leaf, b.leaf + b.n_leaf, a->pass + b.n_inner);
     int64_t pos = 0, units = 0;
     int64_t longest = 0, shortest = INT64_MAX;  // positions of a unit
-    bool fits = true, alike = a->n_inner == 0;
+    bool fits = true, wide = a->n_inner == 0;  // wide: leaves of 128-row tiles with keys, and nothing else
     for (int i = 0; i < a->n_pass; ++i) {
       SeqPass& p = a->pass[i];
       const bool narrow = p.tile_rows == kSubRows;
@@ -319,23 +339,22 @@ int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool 
       units += (int64_t)p.q_tiles * n_heads;
       longest = std::max(longest, per);
       shortest = std::min(shortest, per);
-      alike = alike && !narrow;
+      wide = wide && !narrow && T > 0;
     }
     if (pos > INT32_MAX / 2 || units > INT32_MAX / 2) {
       if (n == 1) return 0;
       continue;
     }
-    alike = alike && shortest > 0 && longest * 4 <= shortest * 5;
     // The device's workgroup slots.  (With inner passes an XCD's two shares are rounded up each: a workgroup more
     // than its slots would wait for a whole chunk.)
     const int at_once = std::max(1, kAttnWgPerCu * n_cus - (a->n_inner > 0 ? a->n_queues : 0));
-    a->rounds = alike ? (int)(units / at_once) : 0;
+    a->rounds = wide ? whole_rounds(*a, units, pos, at_once) : 0;
     a->width = at_once;
     a->total = (int)pos;
     const int first = a->rounds * at_once;  // the first unit that is cut
     a->pos_first = first == 0 ? 0 : first < units ? first_pos(*a, first) : a->total;
     a->E = (int)std::max<int64_t>(kMinChunk, ceil_div64(a->total - a->pos_first, at_once));
-    if (alike && longest == shortest && first < units) {
+    if (wide && longest == shortest && first < units) {
       // units of one length in equal pieces: a tile takes `pieces` positions and a chunk as many as a unit has tiles
       const int64_t T = seq_tiles(a->pass[0]), even = ceil_div64((units - first) * T, at_once);
       int64_t pieces = std::min<int64_t>(at_once / (units - first), std::max<int64_t>(1, T * kWideCost / kMinChunk));
