@@ -494,10 +494,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void seq_fwd_kernel(SeqArgs a) {
       narrow_segment(a, p, tc, g, lds, s_m, s_l);
     } else {
       // The sums over a segment's keys take any order.  The chunks of a head cover different keys; the one that has
-      // worked for i tiles takes tile i modulo the chunk's length where its segment holds it, so that they are at the
-      // same few tiles at a time and find them in their XCD's L2.  (In key order each fetched its keys from beyond
-      // it, and that was the bound: 1041 queries over 52,000 rows 342 -> 322 us.)
-      const int per = uniform(max(1, a.E / p.cost));
+      // worked for i tiles takes tile i modulo the chunk's length (or the unit's, where that is less) if its segment
+      // holds it, so that they are at the same few tiles at a time and find them in their XCD's L2.  (In key order
+      // each fetched its keys from beyond it, and that was the bound: 1041 queries over 52,000 rows 342 -> 322 us.)
+      const int per = uniform(max(1, min(a.E / p.cost, T)));
       const int ahead = uniform((done - g.t0) % per);
       g.ts = g.t0 + (ahead < 0 ? ahead + per : ahead);
       if (whole || g.ts >= g.t1) g.ts = g.t0;
