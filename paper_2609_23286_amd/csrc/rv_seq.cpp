@@ -210,9 +210,9 @@ int first_pos(const SeqArgs& a, int64_t u) {
 
 // Rounds of whole units, one to each of `width` workgroups: as many as the units fill, unless the one whose units are
 // the longest would work kWholeMore percent longer than with all units cut into equal chunks.  (16 frames of 1041
-// tokens over 5100 to 6000 rows of their own: whole units 598 us, chunks 733; over 750 to 6000 rows 413 and 466.  4
-// frames, a round of 3.5 of them: over 4200 to 6000 rows, 10 % longer, 154 and 159; 3000 to 6000, 19 %, 149 and 148; 600
-// to 6000, 40 %, 145 and 115.)
+// tokens over 5100 to 6000 rows of their own: whole units 570 us, chunks 684; over 750 to 6000 rows 410 and 461.  4
+// frames, a round of 3.5 of them: over 4200 to 6000 rows, 10 % longer, 154 and 159; 3000 to 6000, 19 %, 148 and 147;
+// 600 to 6000, 40 %, 145 and 116.)
 constexpr int kWholeMore = 15;
 int whole_rounds(const SeqArgs& a, int64_t units, int64_t total, int width) {
   const int rounds = (int)(units / width);
