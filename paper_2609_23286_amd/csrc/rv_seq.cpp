@@ -289,13 +289,11 @@ struct Builder {
       a->pass[n_inner] = make(i, j, p0, shared, parent);
       parent = n_inner++;
       p0 = shared;
-    } else if (shared > p0) {  // not worth a pass: every sequence takes these pages by itself
-      for (int k = i; k < j; ++k) build(k, k + 1, p0, parent);
-      return;
     }
+    // Neighbours that have more in common go on together; pages that were not worth a pass above begin theirs.
     for (int k = i; k < j;) {
       int e = k + 1;
-      while (e < j && common[e - 1] > p0) ++e;
+      while (e < j && common[e - 1] > shared) ++e;
       build(k, e, p0, parent);
       k = e;
     }

@@ -1,0 +1,96 @@
+// Host checks of the plans of an attention over sequences: what they read.
+#include <algorithm>
+#include <cstdarg>
+#include <cstdio>
+#include <vector>
+
+#include "../../paper_2609_23286_amd/csrc/rv_ops.h"
+
+namespace {
+int g_fail = 0;
+__attribute__((format(printf, 2, 3))) void check(bool ok, const char* fmt, ...) {
+  if (ok || ++g_fail >= 20) return;
+  va_list ap;
+  va_start(ap, fmt);
+  std::vfprintf(stderr, fmt, ap);
+  va_end(ap);
+  std::fputc('\n', stderr);
+}
+
+using rv::PageBook;
+
+int grown(PageBook& book, int parent, int64_t keep, int64_t rows) {  // a fork of `keep` rows, `rows` appended
+  const int s = book.open();
+  if (parent >= 0) book.fork(s, parent, keep);
+  book.append(s, rows);
+  book.release_dropped();
+  return s;
+}
+
+rv::SeqArgs plan(const PageBook& book, const std::vector<int>& seqs, int tokens, bool frame, int n_heads, int group,
+                 int* done) {
+  std::vector<rv::SeqSpan> span;
+  for (int s : seqs) span.push_back({s, tokens});
+  rv::SeqArgs a{};
+  a.n_queues = 8;
+  *done = rv::plan_seqs(book, span.data(), (int)span.size(), 0, frame, n_heads, group, 256, 8192, &a);
+  return a;
+}
+
+// Key tiles of pages that a head's units of all passes go over.
+int64_t tiles(const rv::SeqArgs& a) {
+  int64_t n = 0;
+  for (int i = 0; i < a.n_pass; ++i) n += (int64_t)a.pass[i].q_tiles * a.pass[i].n_pages;
+  return n;
+}
+
+// Branches below a root of `levels` short shared stretches, one inside the other, `per` leaves to a branch: however short
+// what they all have in common, a branch's own pages are read once for its leaves, and the root's no more often than
+// once a branch (or in passes of their own, for no more).
+void check_short_roots() {
+  struct Tree { int branches, per, levels; int64_t stretch, trunk; int tokens, group; };
+  std::vector<Tree> trees;
+  for (int64_t root = 0; root <= 512; root += 64)
+    for (int tokens : {1, 5}) {
+      trees.push_back({2, 8, 1, root, 20000, tokens, 1});
+      trees.push_back({3, 4, 1, root, 6000, tokens, 4});
+      trees.push_back({4, 4, 2, root, 9000, tokens, 1});
+      trees.push_back({5, 3, 4, root / 2, 5000, tokens, 2});
+    }
+  for (const Tree& t : trees) {
+    PageBook book;
+    check(book.init(20000, 200, 1000), "init");
+    // (levels: branch b leaves the root after min(b + 1, levels) stretches)
+    const int root = grown(book, -1, 0, t.levels * t.stretch);
+    std::vector<int> with, without;
+    int64_t root_pages = 0;
+    for (int b = 0; b < t.branches; ++b) {
+      const int64_t keep = std::min(b + 1, t.levels) * t.stretch;
+      const int trunk = grown(book, root, keep, t.trunk), bare = grown(book, -1, 0, t.trunk);
+      root_pages += (keep + 63) / 64;
+      for (int k = 0; k < t.per; ++k) {
+        with.push_back(grown(book, trunk, keep + t.trunk, 20 * k));
+        without.push_back(grown(book, bare, t.trunk, 20 * k));
+      }
+    }
+    int n, m;
+    const rv::SeqArgs a = plan(book, with, t.tokens, true, 16, t.group, &n);
+    const rv::SeqArgs b = plan(book, without, t.tokens, true, 16, t.group, &m);
+    check(n == (int)with.size() && m == (int)without.size(), "one launch");
+    // a trunk behind a root that ends inside a page may take a page more, in each leaf's and the branch's passes
+    const int64_t most = tiles(b) + root_pages + t.branches * (t.per + 1);
+    check(tiles(a) <= most, "%d branches of %d, root of %d x %lld rows, %d tokens: %lld tiles, at most %lld (%d inner passes)",
+          t.branches, t.per, t.levels, (long long)t.stretch, t.tokens, (long long)tiles(a), (long long)most, a.n_inner);
+  }
+}
+}  // namespace
+
+int main() {
+  check_short_roots();
+  if (g_fail) {
+    std::fprintf(stderr, "%d checks failed\n", g_fail);
+    return 1;
+  }
+  std::printf("sequence plans OK\n");
+  return 0;
+}
