@@ -451,7 +451,8 @@ rv_status rv_pool_compact(rv_pool p, int n, const int *seqs, const int64_t *firs
  * natural log.  A query without any key gets out 0 and lse -infinity.  Pages that neighbours in
  * `seqs` have in common are read once for the queries of all of them where that saves work: name forks of one
  * sequence next to each other.  A sequence may be named more than once.
- * n_tokens[i] in [0, 16384].  Arithmetic as rv_attend_frame; results do not depend on what else is in the
+ * n_tokens[i] in [0, 16384], and for each i alone: n_heads times the query tiles (128 rows each, of n_tokens[i] g) times
+ * the key tiles (64 rows each, rows and frame keys apart) plus 4 below 2^28 (RV_ERR_INVALID).  Arithmetic as rv_attend_frame; results do not depend on what else is in the
  * batch beyond its rounding.  Allocates nothing and does not synchronise. */
 rv_status rv_attend_seqs(rv_pool p, int n, const int *seqs, const int *n_tokens, const void *Q, const void *K,
                          const void *V, int n_q_heads, void *out, float *lse, void *stream);

@@ -296,9 +296,16 @@ struct SeqSpan {  // one sequence of a batch, as the plan sees it
   int n_tok;
 };
 
-// Plans one launch for sequences [0, n) of a batch (tokens packed in order, the first at tok0):
-// fills a's passes, returns how many of the sequences it covers (>= 1).
-// 0 if the first one alone is too large.
+// Rows of a query tile of a pass of q_rows (token, query head of the group) rows.
+RV_HD inline int seq_tile_rows(int64_t q_rows) { return q_rows <= kSubRows ? kSubRows : kAttnBQ; }
+
+// Whether one sequence's queries fit a launch, whose positions are 32-bit numbers: its units, each of its key tiles
+// and kSeqTilesMore, come to fewer than kMaxSeqTiles.
+constexpr int64_t kMaxSeqTiles = (int64_t)1 << 28, kSeqTilesMore = 4;
+bool seq_fits(int64_t rows, int n_tok, bool frame, int n_heads, int group);
+
+// Plans one launch for sequences [0, n) of a batch (tokens packed in order, the first at tok0), each of which
+// fits: fills a's passes, returns how many of the sequences it covers (>= 1).
 int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool frame, int n_heads, int group,
               int n_cus, int64_t max_slots, SeqArgs* a);
 

@@ -430,6 +430,9 @@ rv_status rv_attend_seqs(rv_pool p, int n, const int* seqs, const int* n_tokens,
   if (total > INT32_MAX / 2) return fail(RV_ERR_INVALID, "too many tokens for one call");
   if (!K != !V) return fail(RV_ERR_INVALID, "K and V must both be given or both be NULL");
   if (total == 0) return RV_OK;
+  for (int i = 0; i < n; ++i)  // (all of them before the first launch)
+    if (!rv::seq_fits(p->book.len(seqs[i]), n_tokens[i], K != nullptr, p->n_heads, n_q_heads / p->n_heads))
+      return fail(RV_ERR_INVALID, "sequence %d: too many tokens over too many rows for one call", seqs[i]);
   if (!Q || !out || !lse) return fail(RV_ERR_INVALID, "Q, out and lse are required");
   if (!aligned(Q) || !aligned(K) || !aligned(V) || !aligned(out))
     return fail(RV_ERR_INVALID, "Q, K, V and out must be 16-byte aligned");
@@ -461,7 +464,6 @@ rv_status rv_attend_seqs(rv_pool p, int n, const int* seqs, const int* n_tokens,
     if (m == 0) break;
     const int done = rv::plan_seqs(p->book, span, m, tok0, K != nullptr, p->n_heads, a.group, ctx.n_cus,
                                    (int64_t)(ctx.seq_floats / rv::kSubFloats), &a);
-    if (done == 0) return fail(RV_ERR_INVALID, "sequence %d: too many tokens over too many rows for one call", span[0].seq);
     RV_HIP(rv::launch_attend_seqs(a, (hipStream_t)stream), "attention launch");
     for (int k = 0; k < done; ++k) tok0 += span[k].n_tok;
     i = at[done - 1] + 1;

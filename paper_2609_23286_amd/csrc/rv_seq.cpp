@@ -187,6 +187,9 @@ int common_pages(const PageBook& book, int a, int b) {
 // batches lost 10 to 40 %.)
 constexpr int kWideCost = 4, kWideFixed = 16, kNarrowCost = 2, kNarrowFixed = 16;
 constexpr int kMinChunk = 20;     // positions
+// (a sequence that fits takes no more positions than a plan may have)
+static_assert(kWideCost * kMaxSeqTiles <= INT32_MAX / 2 + 1 && kWideFixed <= kWideCost * kSeqTilesMore &&
+              kNarrowCost <= kWideCost && kNarrowFixed <= kWideCost * kSeqTilesMore, "positions");
 // (no chunk between a unit's first and last is without a tile of it)
 static_assert(kMinChunk >= kWideFixed + kWideCost && kMinChunk >= kNarrowFixed + kNarrowCost, "chunk length");
 // Where all units have one length, they are cut into equal pieces, so that the query tiles of a head go over the
@@ -241,9 +244,7 @@ struct Builder {
   bool overflow;
 
   int64_t tiles(int64_t n_tok) const { return ceil_div64(n_tok * group, tile_rows(n_tok)); }
-  int tile_rows(int64_t n_tok) const {
-    return n_tok * group <= kSubRows ? kSubRows : kAttnBQ;
-  }
+  int tile_rows(int64_t n_tok) const { return seq_tile_rows(n_tok * group); }
 
   SeqPass make(int i, int j, int p0, int p1, int parent) const {
     SeqPass p{};
@@ -302,6 +303,12 @@ struct Builder {
 
 }  // namespace
 
+bool seq_fits(int64_t rows, int n_tok, bool frame, int n_heads, int group) {
+  const int64_t q_rows = (int64_t)n_tok * group, units = ceil_div64(q_rows, seq_tile_rows(q_rows)) * n_heads;
+  const int64_t T = ceil_div64(rows, kPageRows) + (frame ? ceil_div64(n_tok, kAttnBK) : 0);
+  return units * (T + kSeqTilesMore) < kMaxSeqTiles;
+}
+
 int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool frame, int n_heads, int group,
               int n_cus, int64_t max_slots, SeqArgs* a) {
   n = std::min(n, kMaxPasses - 1);
@@ -339,10 +346,7 @@ int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool 
       shortest = std::min(shortest, per);
       wide = wide && !narrow && T > 0;
     }
-    if (pos > INT32_MAX / 2 || units > INT32_MAX / 2) {
-      if (n == 1) return 0;
-      continue;
-    }
+    if (n > 1 && (pos > INT32_MAX / 2 || units > INT32_MAX / 2)) continue;
     // The device's workgroup slots.  (With inner passes an XCD's two shares are rounded up each: a workgroup more
     // than its slots would wait for a whole chunk.)
     const int at_once = std::max(1, kAttnWgPerCu * n_cus - (a->n_inner > 0 ? a->n_queues : 0));

@@ -1,5 +1,6 @@
-// Host checks of the plans of an attention over sequences: what they read.
+// Host checks of the plans of an attention over sequences: what they read, and the largest ones.
 #include <algorithm>
+#include <climits>
 #include <cstdarg>
 #include <cstdio>
 #include <vector>
@@ -83,10 +84,41 @@ void check_short_roots() {
           t.branches, t.per, t.levels, (long long)t.stretch, t.tokens, (long long)tiles(a), (long long)most, a.n_inner);
   }
 }
+// The largest sequences that fit are planned whole and within 32 bits, alone and several together; larger ones do not fit.
+void check_largest() {
+  struct Size { int tokens, n_heads, group; bool frame; };
+  for (const Size& z : {Size{16384, 1, 1024, false}, Size{16384, 16, 8, true}, Size{16384, 1024, 1, false},
+                        Size{1041, 16, 1, true}, Size{1, 2, 4, false}, Size{129, 3, 1, true}}) {
+    const int64_t q_rows = (int64_t)z.tokens * z.group, units = (q_rows + 127) / 128 * z.n_heads;
+    const int64_t frame = z.frame ? (z.tokens + 63) / 64 : 0, most = ((int64_t)1 << 28) / units;
+    const int64_t pages = (most * units < (int64_t)1 << 28 ? most : most - 1) - 4 - frame;  // units (pages + frame + 4) < 2^28
+    check(rv::seq_fits(pages * 64, z.tokens, z.frame, z.n_heads, z.group), "%d tokens over %lld pages fit", z.tokens, (long long)pages);
+    check(!rv::seq_fits(pages * 64 + 1, z.tokens, z.frame, z.n_heads, z.group), "%d tokens over %lld pages and a row do not", z.tokens,
+          (long long)pages);
+    if (pages > 4000000) continue;  // (more than a device holds)
+    PageBook book;
+    check(book.init((int)pages * 2, 2, (int)pages), "init");
+    const std::vector<int> seqs = {grown(book, -1, 0, pages * 64), grown(book, -1, 0, pages * 64 - 1)};
+    for (int n = 1; n <= 2; ++n) {
+      int done;
+      const rv::SeqArgs a = plan(book, std::vector<int>(seqs.begin(), seqs.begin() + n), z.tokens, z.frame, z.n_heads, z.group, &done);
+      check(done >= 1 && a.n_inner == 0 && a.n_pass == done, "sequences planned");
+      int64_t pos = 0;
+      for (int i = 0; i < done; ++i) {
+        const rv::SeqPass& p = a.pass[i];
+        check(p.n_pages == pages && p.pos0 == pos, "pass %d", i);
+        pos += (int64_t)p.q_tiles * z.n_heads * (p.fixed + (int64_t)rv::seq_tiles(p) * p.cost);
+      }
+      check(pos == a.total && a.total > 0 && a.E > 0 && a.pos_first >= 0 && (int64_t)a.pos_first + (int64_t)a.chunks * a.E < INT32_MAX,
+            "positions within 32 bits");
+    }
+  }
+}
 }  // namespace
 
 int main() {
   check_short_roots();
+  check_largest();
   if (g_fail) {
     std::fprintf(stderr, "%d checks failed\n", g_fail);
     return 1;
