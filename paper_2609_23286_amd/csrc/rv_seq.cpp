@@ -403,7 +403,8 @@ int plan_seqs(const PageBook& book, const SeqSpan* spans, int n, int tok0, bool 
       if (shared || most > 1) merge += ceil_div64((int64_t)p.n_tok * group, p.merge_rows) * n_heads;
     }
     a->merge_blocks = (int)merge;
-    if (n == 1 || (fits && slots <= max_slots)) return n;
+    // (one sequence's join takes 16384 x 1024 / 4 workgroups at most)
+    if (n == 1 || (fits && slots <= max_slots && merge <= kMaxGridBlocks)) return n;
   }
 }
 

@@ -114,11 +114,34 @@ void check_largest() {
     }
   }
 }
+// The merge launch stays within what a grid holds, however many rows the batch has.
+void check_merge_grid() {
+  PageBook book;
+  check(book.init(200, 60, 10), "init");
+  std::vector<int> seqs;
+  for (int i = 0; i < 50; ++i) seqs.push_back(grown(book, -1, 0, 128));
+  for (int tokens : {16384, 5000, 1}) {
+    std::vector<rv::SeqSpan> span;
+    for (int s : seqs) span.push_back({s, tokens});
+    span.push_back({seqs[0], 1});  // (few queries: the others' units are cut)
+    int tok0 = 0;
+    for (size_t i = 0; i < span.size();) {
+      rv::SeqArgs a{};
+      a.n_queues = 8;
+      const int done = rv::plan_seqs(book, &span[i], (int)(span.size() - i), tok0, false, 1024, 1, 256, 8192, &a);
+      check(done >= 1, "sequences planned");
+      check(a.merge_blocks <= rv::kMaxGridBlocks, "%d sequences of %d tokens: %d workgroups join", done, tokens, a.merge_blocks);
+      for (int k = 0; k < done; ++k) tok0 += span[i + k].n_tok;
+      i += done;
+    }
+  }
+}
 }  // namespace
 
 int main() {
   check_short_roots();
   check_largest();
+  check_merge_grid();
   if (g_fail) {
     std::fprintf(stderr, "%d checks failed\n", g_fail);
     return 1;

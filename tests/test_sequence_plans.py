@@ -1,4 +1,4 @@
-"""The plans of attentions over sequences, under sanitizers: what a launch reads, and the largest launches."""
+"""The plans of attentions over sequences, under sanitizers: what a launch reads, the largest launches and their grids."""
 import os
 
 from test_sanitizers import NATIVE, ROOT, SAN, build_and_run
