@@ -362,7 +362,7 @@ __device__ __forceinline__ float fold8(float x, float y, bool upper) {
 template <bool F32, int AXES, bool ONE>
 __global__ __launch_bounds__(NT) void prepare_bwd_kernel(PrepArgs a) {
   __shared__ __attribute__((aligned(16))) float2 s_angles[NW][kPrepMaxTokens * D];
-  __shared__ float s_sum[NW][4 * D];
+  __shared__ __attribute__((aligned(16))) float s_sum[NW][4 * D];
   __shared__ __attribute__((aligned(16))) float s_vec[4 * D];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Cols<F32> c = lane_cols<F32, AXES>(lane);
