@@ -496,9 +496,17 @@ class QKVPrep:
             if t is not None and t.dtype != torch.float32:
                 raise TypeError(f"{name}: dtype {t.dtype}, expected torch.float32")
         ptrs = [_ptr(t, (HEAD_DIM,), 4, "weight or bias") for t in self.vectors]
+        devices = {t.get_device() for t in self.vectors if t is not None}
+        if len(devices) > 1:
+            raise ValueError("weights and biases on different devices")
+        self.device = devices.pop() if devices else None
         self.c = rv_qkv_prep(n_q_heads, n_kv_heads, _NORMS[norm], axes, eps, base, *ptrs)
         self.n_q_heads, self.n_kv_heads, self.axes = n_q_heads, n_kv_heads, axes
         self._args = (ctypes.addressof(self.c), axes, n_q_heads, n_kv_heads)
+
+    def _check_device(self, device):
+        if self.device is not None and self.device != device:
+            raise ValueError(f"weights and biases on device {self.device} while device {device} is current")
 
 
 def _rows(t, heads, what):
@@ -552,9 +560,10 @@ def prepare_qkv(prep, q, k, v, pos, Q, K, V, stream=None):
     """rv_prepare_qkv: q [N, Hq * 64], k, v [N, Hk * 64] (bf16 or fp32, rows at any distance) to the frame
     tensors Q [N, Hq, 64], K, V [N, Hk, 64] bf16; pos [N, axes] int32.  v and V may be None."""
     device, s = _where(stream)
+    prep._check_device(device)
     if _made(_bind.prepare(*prep._args, device, s, q, k, v, pos, Q, K, V)):
         return
-    _same_device(device, q, k, v, pos, Q, K, V, *prep.vectors)
+    _same_device(device, q, k, v, pos, Q, K, V)
     N, Hq, Hk = q.shape[0], prep.n_q_heads, prep.n_kv_heads
     src, dtype = _prep_rows(((q, Hq, "q"), (k, Hk, "k"), (v, Hk, "v")), N)
     _check(_lib.rv_prepare_qkv(ctypes.byref(prep.c), *src, dtype, N, _positions(prep, pos, N),
@@ -564,7 +573,9 @@ def prepare_qkv(prep, q, k, v, pos, Q, K, V, stream=None):
 
 def stage_qkv(prep, q, k, v, pos, Q, mem, stream=None):
     """rv_mem_stage_qkv: prepare_qkv whose K and V become the frame staged in mem."""
-    _same_device(torch.cuda.current_device(), q, k, v, pos, Q, *prep.vectors)
+    device = torch.cuda.current_device()
+    prep._check_device(device)
+    _same_device(device, q, k, v, pos, Q)
     N, Hq, Hk = q.shape[0], prep.n_q_heads, prep.n_kv_heads
     src, dtype = _prep_rows(((q, Hq, "q"), (k, Hk, "k"), (v, Hk, "v")), N)
     _check(_lib.rv_mem_stage_qkv(mem.handle, ctypes.byref(prep.c), *src, dtype, N, _positions(prep, pos, N),
@@ -577,10 +588,11 @@ def prepare_qkv_bwd(prep, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight=None, dq_
     distance) and, where given, of the weights and biases ([64] fp32, overwritten), from dQ [N, Hq, 64]
     and dK, dV [N, Hk, 64] bf16.  dV and dv may be None."""
     device, s = _where(stream)
+    prep._check_device(device)
     if _made(_bind.prepare_bwd(*prep._args, device, s, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight, dq_bias,
                                dk_weight, dk_bias)):
         return
-    _same_device(device, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight, dq_bias, dk_weight, dk_bias, *prep.vectors)
+    _same_device(device, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight, dq_bias, dk_weight, dk_bias)
     N, Hq, Hk = q.shape[0], prep.n_q_heads, prep.n_kv_heads
     rows, dtype = _prep_rows(((q, Hq, "q"), (k, Hk, "k"), (dq, Hq, "dq"), (dk, Hk, "dk"), (dv, Hk, "dv")), N)
     sums = []
