@@ -176,6 +176,7 @@ decltype(&rv_pool_compact) g_compact = nullptr;
 decltype(&rv_attend_seqs) g_attend = nullptr;
 
 constexpr int64_t kHeadDim = 64;
+constexpr c10::ScalarType kBF16 = c10::ScalarType::BFloat16;
 
 // Arguments read one after another; `plain` turns false at the first that is not as expected.
 class Args {
@@ -231,13 +232,14 @@ class Args {
       return plain = false, nullptr;
     return &t;
   }
-  // Its address, if contiguous with elements of `itemsize` bytes (of `type`, where given) and this shape;
-  // d[0] < 0: any shape of -d[0] - 1 elements.
-  void* exact(int64_t device, int itemsize, std::initializer_list<int64_t> d, c10::ScalarType type = c10::ScalarType::Undefined) {
+  // Its address, if contiguous, of `type` (BFloat16: or its bits as whole numbers) and of this shape; d[0] < 0: any
+  // shape of -d[0] - 1 elements.
+  void* exact(int64_t device, c10::ScalarType type, std::initializer_list<int64_t> d) {
     const at::Tensor* t = tensor(device);
     if (!t) return nullptr;
-    bool ok = t->is_contiguous() && (int64_t)t->element_size() == itemsize &&
-              (type == c10::ScalarType::Undefined || t->scalar_type() == type);
+    const c10::ScalarType ty = t->scalar_type();
+    bool ok = t->is_contiguous() && (ty == type || (type == c10::ScalarType::BFloat16 &&
+                                                    (ty == c10::ScalarType::Short || ty == c10::ScalarType::UInt16)));
     if (*d.begin() < 0) {
       ok = ok && t->numel() == -*d.begin() - 1;
     } else {
@@ -308,9 +310,9 @@ PyObject* py_prepare(PyObject*, PyObject* const* args, Py_ssize_t n) {
     c10::ScalarType ty = c10::ScalarType::Undefined;
     void *q = a.rows(dev, hq, &N, &ty, &sq), *k = a.rows(dev, hk, &N, &ty, &sk), *v = a.rows(dev, hk, &N, &ty, &sv);
     if (!q || N > INT32_MAX) a.plain = false;
-    void* pos = a.exact(dev, 4, {N, axes}, c10::ScalarType::Int);
-    void *Q = a.exact(dev, 2, {N, hq, kHeadDim}), *K = a.exact(dev, 2, {N, hk, kHeadDim}),
-         *V = a.exact(dev, 2, {N, hk, kHeadDim});
+    void* pos = a.exact(dev, c10::ScalarType::Int, {N, axes});
+    void *Q = a.exact(dev, kBF16, {N, hq, kHeadDim}), *K = a.exact(dev, kBF16, {N, hk, kHeadDim}),
+         *V = a.exact(dev, kBF16, {N, hk, kHeadDim});
     return made(a.plain && !(axes == 0 && pos), [&] {
       return g_prepare(prep, q, sq, k, sk, v, sv, dtype_of(ty), (int)N, (const int32_t*)pos, Q, K, V, s);
     });
@@ -330,12 +332,12 @@ PyObject* py_prepare_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
     c10::ScalarType ty = c10::ScalarType::Undefined;
     void *q = a.rows(dev, hq, &N, &ty, &sq), *k = a.rows(dev, hk, &N, &ty, &sk);
     if (!q || N > INT32_MAX) a.plain = false;
-    void* pos = a.exact(dev, 4, {N, axes}, c10::ScalarType::Int);
-    void *dQ = a.exact(dev, 2, {N, hq, kHeadDim}), *dK = a.exact(dev, 2, {N, hk, kHeadDim}),
-         *dV = a.exact(dev, 2, {N, hk, kHeadDim});
+    void* pos = a.exact(dev, c10::ScalarType::Int, {N, axes});
+    void *dQ = a.exact(dev, kBF16, {N, hq, kHeadDim}), *dK = a.exact(dev, kBF16, {N, hk, kHeadDim}),
+         *dV = a.exact(dev, kBF16, {N, hk, kHeadDim});
     void *dq = a.rows(dev, hq, &N, &ty, &tq), *dk = a.rows(dev, hk, &N, &ty, &tk), *dv = a.rows(dev, hk, &N, &ty, &tv);
     float* sums[4];
-    for (float*& x : sums) x = (float*)a.exact(dev, 4, {kHeadDim}, c10::ScalarType::Float);
+    for (float*& x : sums) x = (float*)a.exact(dev, c10::ScalarType::Float, {kHeadDim});
     return made(a.plain && !(axes == 0 && pos), [&] {
       return g_prepare_bwd(prep, q, sq, k, sk, dtype_of(ty), (int)N, (const int32_t*)pos, dQ, dK, dV, dq, tq, dk, tk, dv,
                            tv, sums[0], sums[1], sums[2], sums[3], s);
@@ -395,7 +397,7 @@ PyObject* py_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
     r.integers(&rows);
     if (!r.plain || rows.size() != seqs.size()) a.plain = false;
     const int64_t total = sum(rows);
-    void *K = a.exact(dev, 2, {total, H, kHeadDim}), *V = a.exact(dev, 2, {total, H, kHeadDim});
+    void *K = a.exact(dev, kBF16, {total, H, kHeadDim}), *V = a.exact(dev, kBF16, {total, H, kHeadDim});
     return made(a.plain, [&] { return g_append((rv_pool)pool, (int)seqs.size(), seqs.data(), K, V, rows.data(), s); });
   });
 }
@@ -416,7 +418,7 @@ PyObject* py_gather(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (rows.size() != seqs.size() || (has_first && first.size() != seqs.size())) a.plain = false;
     const int64_t size = sum(rows) * H * kHeadDim;
     if (size < 0) a.plain = false;
-    void *K = a.exact(dev, 2, {-size - 1}), *V = a.exact(dev, 2, {-size - 1});
+    void *K = a.exact(dev, kBF16, {-size - 1}), *V = a.exact(dev, kBF16, {-size - 1});
     return made(a.plain, [&] {
       return g_gather((rv_pool)pool, (int)seqs.size(), seqs.data(), has_first ? first.data() : nullptr, rows.data(), K, V, s);
     });
@@ -439,7 +441,7 @@ PyObject* py_compact(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (keeps.size() != seqs.size() || (has_first && first.size() != seqs.size())) a.plain = false;
     const int64_t size = sum(keeps) * H;
     if (size < 0) a.plain = false;
-    void* keep = a.exact(dev, 4, {-size - 1}, c10::ScalarType::Int);
+    void* keep = a.exact(dev, c10::ScalarType::Int, {-size - 1});
     return made(a.plain, [&] {
       return g_compact((rv_pool)pool, (int)seqs.size(), seqs.data(), has_first ? first.data() : nullptr, keeps.data(),
                        (const int32_t*)keep, s);
@@ -462,9 +464,9 @@ PyObject* py_attend(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int64_t total = sum(tokens);
     if (!a.plain || total < 0 || THPVariable_Unpack(args[6]).dim() != 3) Py_RETURN_NONE;
     const int64_t hq = THPVariable_Unpack(args[6]).size(1);
-    void *Q = a.exact(dev, 2, {total, hq, kHeadDim}), *K = a.exact(dev, 2, {total, H, kHeadDim}),
-         *V = a.exact(dev, 2, {total, H, kHeadDim}), *out = a.exact(dev, 2, {total, hq, kHeadDim});
-    void* lse = a.exact(dev, 4, {-total * hq - 1});
+    void *Q = a.exact(dev, kBF16, {total, hq, kHeadDim}), *K = a.exact(dev, kBF16, {total, H, kHeadDim}),
+         *V = a.exact(dev, kBF16, {total, H, kHeadDim}), *out = a.exact(dev, kBF16, {total, hq, kHeadDim});
+    void* lse = a.exact(dev, c10::ScalarType::Float, {-total * hq - 1});
     return made(a.plain && hq == (int)hq, [&] {
       return g_attend((rv_pool)pool, (int)seqs.size(), seqs.data(), tokens.data(), Q, K, V, (int)hq, out, (float*)lse, s);
     });

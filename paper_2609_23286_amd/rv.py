@@ -4,8 +4,9 @@ Every step of the hot path runs in librv's HIP kernels; this module checks tenso
 shapes/dtypes/devices the C ABI cannot see (it receives raw pointers), converts
 handles, and raises RVError on any non-zero rv_status.  Tensors are torch CUDA
 (HIP) tensors; bf16 tensors may be any 2-byte dtype (bfloat16, int16, uint16) since
-only their bits matter.  PyTorch supplies device memory and streams, nothing else.
-There is no fallback: if librv.so or the marshalling module _rv_bind.so is missing the
+only their bits matter (the calls for projections and sequences refuse others, float16
+among them; the per-frame ones look at the size alone).  PyTorch supplies device memory
+and streams, nothing else.  There is no fallback: if librv.so or the marshalling module _rv_bind.so is missing the
 import of this module fails.
 """
 import ctypes
@@ -195,6 +196,28 @@ def _made(status):
     if status != RV_OK:
         _check(status)
     return True
+
+
+_BF16_BITS = (torch.bfloat16, torch.int16, torch.uint16)
+
+
+def _typed(t, types, shape, what):
+    if isinstance(t, torch.Tensor) and t.dtype not in types:
+        raise TypeError(f"{what}: dtype {t.dtype}, expected {types[0]}")
+    return _ptr(t, shape, types[0].itemsize, what)
+
+
+def _bf16(t, shape, what):
+    """_ptr of bf16 values, or of their bits as whole numbers."""
+    return _typed(t, _BF16_BITS, shape, what)
+
+
+def _fp32(t, shape, what):
+    return _typed(t, (torch.float32,), shape, what)
+
+
+def _int32(t, shape, what):
+    return _typed(t, (torch.int32,), shape, what)
 
 
 def _where(stream):
@@ -492,10 +515,8 @@ class QKVPrep:
         if norm not in _NORMS:
             raise ValueError(f"norm: {norm!r} is not one of None, 'rms', 'layer'")
         self.vectors = (q_weight, q_bias, k_weight, k_bias)  # (kept alive: the struct holds addresses)
-        for t, name in zip(self.vectors, ("q_weight", "q_bias", "k_weight", "k_bias")):
-            if t is not None and t.dtype != torch.float32:
-                raise TypeError(f"{name}: dtype {t.dtype}, expected torch.float32")
-        ptrs = [_ptr(t, (HEAD_DIM,), 4, "weight or bias") for t in self.vectors]
+        ptrs = [_fp32(t, (HEAD_DIM,), name)
+                for t, name in zip(self.vectors, ("q_weight", "q_bias", "k_weight", "k_bias"))]
         devices = {t.get_device() for t in self.vectors if t is not None}
         if len(devices) > 1:
             raise ValueError("weights and biases on different devices")
@@ -526,7 +547,7 @@ def _rows(t, heads, what):
         raise ValueError(f"{what}: the elements of a row must be contiguous")
     if t.dtype == torch.float32:
         dtype = RV_F32
-    elif t.element_size() == 2 and t.dtype != torch.float16:
+    elif t.dtype in _BF16_BITS:
         dtype = RV_BF16
     else:
         raise TypeError(f"{what}: dtype {t.dtype}, expected bfloat16 or float32")
@@ -551,9 +572,7 @@ def _prep_rows(ts, n):
 def _positions(prep, pos, n):
     if prep.axes == 0:
         return None
-    if pos is not None and pos.dtype != torch.int32:
-        raise TypeError(f"pos: dtype {pos.dtype}, expected torch.int32")
-    return _ptr(pos, (n,) if prep.axes == 1 and pos is not None and pos.dim() == 1 else (n, prep.axes), 4, "pos")
+    return _int32(pos, (n,) if prep.axes == 1 and pos is not None and pos.dim() == 1 else (n, prep.axes), "pos")
 
 
 def prepare_qkv(prep, q, k, v, pos, Q, K, V, stream=None):
@@ -567,8 +586,8 @@ def prepare_qkv(prep, q, k, v, pos, Q, K, V, stream=None):
     N, Hq, Hk = q.shape[0], prep.n_q_heads, prep.n_kv_heads
     src, dtype = _prep_rows(((q, Hq, "q"), (k, Hk, "k"), (v, Hk, "v")), N)
     _check(_lib.rv_prepare_qkv(ctypes.byref(prep.c), *src, dtype, N, _positions(prep, pos, N),
-                               _ptr(Q, (N, Hq, HEAD_DIM), 2, "Q"), _ptr(K, (N, Hk, HEAD_DIM), 2, "K"),
-                               _ptr(V, (N, Hk, HEAD_DIM), 2, "V"), s))
+                               _bf16(Q, (N, Hq, HEAD_DIM), "Q"), _bf16(K, (N, Hk, HEAD_DIM), "K"),
+                               _bf16(V, (N, Hk, HEAD_DIM), "V"), s))
 
 
 def stage_qkv(prep, q, k, v, pos, Q, mem, stream=None):
@@ -579,7 +598,7 @@ def stage_qkv(prep, q, k, v, pos, Q, mem, stream=None):
     N, Hq, Hk = q.shape[0], prep.n_q_heads, prep.n_kv_heads
     src, dtype = _prep_rows(((q, Hq, "q"), (k, Hk, "k"), (v, Hk, "v")), N)
     _check(_lib.rv_mem_stage_qkv(mem.handle, ctypes.byref(prep.c), *src, dtype, N, _positions(prep, pos, N),
-                                 _ptr(Q, (N, Hq, HEAD_DIM), 2, "Q"), _stream(stream)))
+                                 _bf16(Q, (N, Hq, HEAD_DIM), "Q"), _stream(stream)))
 
 
 def prepare_qkv_bwd(prep, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight=None, dq_bias=None, dk_weight=None,
@@ -595,14 +614,11 @@ def prepare_qkv_bwd(prep, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight=None, dq_
     _same_device(device, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight, dq_bias, dk_weight, dk_bias)
     N, Hq, Hk = q.shape[0], prep.n_q_heads, prep.n_kv_heads
     rows, dtype = _prep_rows(((q, Hq, "q"), (k, Hk, "k"), (dq, Hq, "dq"), (dk, Hk, "dk"), (dv, Hk, "dv")), N)
-    sums = []
-    for t, name in ((dq_weight, "dq_weight"), (dq_bias, "dq_bias"), (dk_weight, "dk_weight"), (dk_bias, "dk_bias")):
-        if t is not None and t.dtype != torch.float32:
-            raise TypeError(f"{name}: dtype {t.dtype}, expected torch.float32")
-        sums.append(_ptr(t, (HEAD_DIM,), 4, name))
+    sums = [_fp32(t, (HEAD_DIM,), name) for t, name in (
+        (dq_weight, "dq_weight"), (dq_bias, "dq_bias"), (dk_weight, "dk_weight"), (dk_bias, "dk_bias"))]
     _check(_lib.rv_prepare_qkv_bwd(ctypes.byref(prep.c), *rows[:4], dtype, N, _positions(prep, pos, N),
-                                   _ptr(dQ, (N, Hq, HEAD_DIM), 2, "dQ"), _ptr(dK, (N, Hk, HEAD_DIM), 2, "dK"),
-                                   _ptr(dV, (N, Hk, HEAD_DIM), 2, "dV"), *rows[4:], *sums, s))
+                                   _bf16(dQ, (N, Hq, HEAD_DIM), "dQ"), _bf16(dK, (N, Hk, HEAD_DIM), "dK"),
+                                   _bf16(dV, (N, Hk, HEAD_DIM), "dV"), *rows[4:], *sums, s))
 
 
 # ---- sequences in pages ----------------------------------------------------------------
@@ -688,7 +704,7 @@ class Pool:
         _same_device(device, K, V)
         n = len(seqs)
         shp = (sum(n_rows), self.n_heads, HEAD_DIM)
-        _check(_lib.rv_pool_append(self.handle, n, _ints(seqs, n, "seqs"), _ptr(K, shp, 2, "K"), _ptr(V, shp, 2, "V"),
+        _check(_lib.rv_pool_append(self.handle, n, _ints(seqs, n, "seqs"), _bf16(K, shp, "K"), _bf16(V, shp, "V"),
                                    _ints(n_rows, n, "n_rows"), s))
 
     def gather(self, seqs, K, V, n_rows, first=None, stream=None):
@@ -704,8 +720,8 @@ class Pool:
                 raise ValueError(f"{what}: {t.numel()} elements, expected {size}")
         _check(_lib.rv_pool_gather(
             self.handle, n, _ints(seqs, n, "seqs"), _ints(first, n, "first", ctypes.c_int64),
-            _ints(n_rows, n, "n_rows", ctypes.c_int64), K if K is None else _ptr(K, tuple(K.shape), 2, "K"),
-            V if V is None else _ptr(V, tuple(V.shape), 2, "V"), s))
+            _ints(n_rows, n, "n_rows", ctypes.c_int64), K if K is None else _bf16(K, tuple(K.shape), "K"),
+            V if V is None else _bf16(V, tuple(V.shape), "V"), s))
 
     def compact(self, seqs, keep, n_keep, first=None, stream=None):
         """rv_pool_compact: seqs[i] keeps its rows before first[i] (default 0) and the n_keep[i] rows of each
@@ -736,8 +752,8 @@ def attend_seqs(Q, K, V, pool, seqs, n_tokens, out, lse, stream=None):
     if lse.numel() != total * Hq:
         raise ValueError(f"lse: {lse.numel()} elements, expected {total * Hq}")
     _check(_lib.rv_attend_seqs(pool.handle, n, _ints(seqs, n, "seqs"), _ints(n_tokens, n, "n_tokens"),
-                               _ptr(Q, shp, 2, "Q"), _ptr(K, kv, 2, "K"), _ptr(V, kv, 2, "V"), Hq,
-                               _ptr(out, shp, 2, "out"), _ptr(lse, tuple(lse.shape), 4, "lse"), s))
+                               _bf16(Q, shp, "Q"), _bf16(K, kv, "K"), _bf16(V, kv, "V"), Hq,
+                               _bf16(out, shp, "out"), _fp32(lse, tuple(lse.shape), "lse"), s))
 
 
 def admit_seqs(Q, K, V, lse, qs, budget, pool, seqs, saliency_out, idx_out, stream=None):
@@ -749,10 +765,10 @@ def admit_seqs(Q, K, V, lse, qs, budget, pool, seqs, saliency_out, idx_out, stre
         raise ValueError(f"Q: {n} frames of {H} heads for {len(seqs)} sequences of {pool.n_heads} heads")
     shp = (n, N, H, d)
     q = qs if isinstance(qs, rv_qsub) else rv_qsub(*qs)
-    _check(_lib.rv_admit_seqs(pool.handle, n, _ints(seqs, n, "seqs"), _ptr(Q, shp, 2, "Q"), _ptr(K, shp, 2, "K"),
-                              _ptr(V, shp, 2, "V"), _ptr(lse, (n, H, N), 4, "lse"), N, ctypes.byref(q), budget,
-                              _ptr(saliency_out, (n, H, N), 4, "saliency_out"),
-                              _ptr(idx_out, (n, H, budget), 4, "idx_out"), _stream(stream)))
+    _check(_lib.rv_admit_seqs(pool.handle, n, _ints(seqs, n, "seqs"), _bf16(Q, shp, "Q"), _bf16(K, shp, "K"),
+                              _bf16(V, shp, "V"), _fp32(lse, (n, H, N), "lse"), N, ctypes.byref(q), budget,
+                              _fp32(saliency_out, (n, H, N), "saliency_out"),
+                              _int32(idx_out, (n, H, budget), "idx_out"), _stream(stream)))
 
 
 # ---- seeded stream generator on the GPU (benchmark inputs) -------------------------
