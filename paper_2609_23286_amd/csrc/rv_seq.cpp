@@ -198,10 +198,14 @@ static_assert(kMinChunk >= kWideFixed + kWideCost && kMinChunk >= kNarrowFixed +
 // 5000 and 10,000 rows three pieces 36, 49 and 76 us, running chunks 44, 56 and 79; over 20,000 the same; over 52,000
 // 319 and 300.  Over 64 rows whole units 22.3 us, three pieces 24.6; over 1000 rows 35 and 31.)
 constexpr int kStartTiles = 16;
-constexpr int kPartialTiles = 5;  // key tiles that a unit's partial result takes as long as
+// Positions that 32 rows of a unit's partial result take as long as, written and joined.  (Pages from which a shared pass
+// was the faster one, measured, and those by the rule: 48 sequences of 5 tokens of 16 heads 14, 13; 16 of a token 13, 12;
+// 8 of 40 tokens 24 to 36, 45; 8 of 130 about 75, 72; 4 of 300 about 240, 221; 12 of 200 about 250, 173.  Away from there:
+// 48 of 5 over 8 pages 29 us shared and 25 apart, over 48 31 and 91; 4 frames of 1041 over 160 pages 282 and 224.)
+constexpr int kPartialCost = 20;
 // Up to which the merge takes a row in 16 lanes, four segments at a time, and above it a wave a row, 16 at a time.
-// (1041 queries over 52,000 rows, five segments: 290 us with 16 lanes, 296 with a wave; four sequences' frames over
-// 5000 shared rows, nine segments: 150 and 154.)
+// (Over 5000 rows of 16 heads, with 16 lanes and with a wave: three segments 47 and 54 us, six 32.5 and 34.8, eight 27.1
+// and 28.7, ten 26.0 both, sixteen 24.4 and 24.0, 31 19.7 and 18.8; over 20,000 rows the same order.)
 constexpr int kFewSegments = 12;
 
 // First position of unit u of all passes' units.
@@ -245,6 +249,9 @@ struct Builder {
 
   int64_t tiles(int64_t n_tok) const { return ceil_div64(n_tok * group, tile_rows(n_tok)); }
   int tile_rows(int64_t n_tok) const { return seq_tile_rows(n_tok * group); }
+  // Positions that a page takes with all the queries of n_tok tokens, and 32-row slots of their partial results.
+  int64_t page_cost(int64_t n_tok) const { return tiles(n_tok) * (tile_rows(n_tok) == kSubRows ? kNarrowCost : kWideCost); }
+  int64_t slots(int64_t n_tok) const { return tiles(n_tok) * (tile_rows(n_tok) / kSubRows); }
 
   SeqPass make(int i, int j, int p0, int p1, int parent) const {
     SeqPass p{};
@@ -276,13 +283,15 @@ struct Builder {
     }
     int shared = common[i];
     for (int k = i + 1; k + 1 < j; ++k) shared = std::min(shared, common[k]);
-    int64_t apart = 0;
-    for (int k = i; k < j; ++k) apart += tiles(spans[k].n_tok);
-    const int64_t joint = tiles(tok[j] - tok[i]);
-    // Worth a pass if it saves more tiles than the partial results cost that every unit then writes
-    // and the merge reads.
-    const int64_t saved = (apart - joint) * (shared - p0);
-    if (saved > kPartialTiles * (apart + joint)) {
+    const int64_t joint_tok = tok[j] - tok[i];
+    int64_t saved = -page_cost(joint_tok), parts = slots(joint_tok);
+    for (int k = i; k < j; ++k) {
+      saved += page_cost(spans[k].n_tok);
+      parts += slots(spans[k].n_tok);
+    }
+    // Worth a pass if it saves more positions than the partial results take that every unit then writes and the
+    // merge reads.
+    if (saved * (shared - p0) > kPartialCost * parts) {
       if (n_leaf + n_inner >= kMaxPasses) {
         overflow = true;
         return;

@@ -136,10 +136,30 @@ void check_merge_grid() {
     }
   }
 }
+// Common pages are a pass of their own where that was measured to be clearly faster, and only there.
+void check_worth() {
+  struct Batch { int seqs, tokens, n_heads, group, pages; bool pass; };
+  for (const Batch& b : {Batch{4, 1041, 16, 1, 160, false}, Batch{16, 1041, 16, 1, 160, false}, Batch{4, 1041, 16, 1, 24, false},
+                         Batch{12, 200, 16, 1, 80, false}, Batch{4, 300, 16, 1, 48, false}, Batch{8, 40, 16, 1, 8, false},
+                         Batch{48, 5, 16, 1, 8, false}, Batch{40, 17, 2, 8, 12, false}, Batch{48, 5, 16, 1, 24, true},
+                         Batch{16, 1, 16, 1, 24, true}, Batch{16, 1, 4, 4, 80, true}, Batch{8, 40, 16, 1, 80, true},
+                         Batch{8, 130, 16, 1, 160, true}, Batch{2, 1, 16, 1, 80, true}, Batch{40, 17, 2, 8, 160, true}}) {
+    PageBook book;
+    check(book.init(2000, 60, 400), "init");
+    const int root = grown(book, -1, 0, b.pages * 64);
+    std::vector<int> seqs;
+    for (int i = 0; i < b.seqs; ++i) seqs.push_back(grown(book, root, b.pages * 64, 300));
+    int done;
+    const rv::SeqArgs a = plan(book, seqs, b.tokens, false, b.n_heads, b.group, &done);
+    check(done == b.seqs && (a.n_inner > 0) == b.pass, "%d sequences of %d tokens over %d pages: %d shared passes", b.seqs,
+          b.tokens, b.pages, a.n_inner);
+  }
+}
 }  // namespace
 
 int main() {
   check_short_roots();
+  check_worth();
   check_largest();
   check_merge_grid();
   if (g_fail) {

@@ -61,10 +61,10 @@ def test_forks_of_a_long_prefix(rv, H, group, tokens):
     w.check_attention(kids, [tokens] * 9, group, frame=tokens > 1)
 
 
-@pytest.mark.parametrize("root", [64, 128, 320, 640])
+@pytest.mark.parametrize("root", [64, 128, 320, 640, 1280])
 @pytest.mark.parametrize("tokens", [1, 5, 150])
 def test_branches_below_a_short_root(rv, root, tokens):
-    """What all share is not worth a pass of its own (but for the longest root): the branches' passes begin with it."""
+    """What all share is not worth a pass of its own (but few tokens over the longest root): the branches' passes begin with it."""
     w = Checked(rv, 2, 300, 40, 5000, seed=root + tokens)
     a = w.open()
     w.append([a], [root])
