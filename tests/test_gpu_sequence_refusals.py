@@ -1,4 +1,6 @@
 """Refusals of the calls around a frame's attention on the GPU: nothing is enqueued, nothing changes."""
+import ctypes
+
 import pytest
 import torch
 
@@ -89,3 +91,19 @@ def test_tensors_of_another_type_of_the_same_size_are_refused(rv):
     rv.prepare_qkv(prep, x, x, x, None, *(bits.clone() for _ in range(3)))
     pool.append([s], bits, bits, [N])
     assert pool.len(s) == 2 * N
+
+
+def test_rows_past_what_a_call_moves_are_refused(rv):
+    """2^28 rows x heads of one sequence; the refusal comes before any page is looked for."""
+    pool = rv.Pool(1024, 4, 2, 1 << 20)
+    s = pool.open()
+    seqs, rows = (ctypes.c_int * 1)(s), (ctypes.c_int * 1)((1 << 18) + 1)
+    L, at = rv.lib(), ctypes.c_void_p(4096)
+    assert L.rv_pool_append(pool.handle, 1, seqs, at, at, rows, None) == rv.RV_ERR_INVALID
+    assert b"too many rows for one call" in L.rv_last_error()
+    keep, first = (ctypes.c_int64 * 1)((1 << 18) + 1), (ctypes.c_int64 * 1)(0)
+    assert L.rv_pool_compact(pool.handle, 1, seqs, first, keep, at, None) == rv.RV_ERR_INVALID
+    assert b"too many rows for one call" in L.rv_last_error()
+    rows[0] = (1 << 20) + 1
+    assert L.rv_pool_append(pool.handle, 1, seqs, at, at, rows, None) == rv.RV_ERR_CAPACITY
+    assert pool.len(s) == 0 and pool.free_pages == 4
