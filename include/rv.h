@@ -354,7 +354,8 @@ typedef struct rv_qkv_prep {
  * row at element 64 h, e.g. column ranges of one fused projection.  v and V may both be NULL.
  * pos: [n_tokens][n_axes] int32 (NULL for n_axes 0).  Q: [n_tokens][n_q_heads][64] bf16; K, V:
  * [n_tokens][n_kv_heads][64] bf16.  Rows and addresses must be 16-byte aligned
- * (RV_ERR_INVALID).  The outputs must not overlap the inputs.  n_tokens 0 is a no-op. */
+ * (RV_ERR_INVALID).  The outputs must not overlap the inputs.  n_tokens 0 is a no-op; up to 2^25 tokens
+ * a call. */
 rv_status rv_prepare_qkv(const rv_qkv_prep *p, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                          const void *v, int64_t v_stride, rv_dtype dtype, int n_tokens, const int32_t *pos,
                          void *Q, void *K, void *V, void *stream);
@@ -370,8 +371,9 @@ rv_status rv_mem_stage_qkv(rv_mem m, const rv_qkv_prep *p, const void *q, int64_
  * laid out as they are (bf16); dq, dk, dv: of `dtype`, rows of dq_stride, ... elements, rounded once.
  * dV and dv may both be NULL.  dq_weight, dq_bias, dk_weight, dk_bias: [64] fp32, overwritten with
  * the sums over tokens and heads, in a fixed order (the same inputs give the same bits); each may be
- * NULL, and must be for RV_NORM_NONE.  n_tokens 0 sets them to zero.  rv_init must have run on the
- * device: the sums' partial results lie in its workspace. */
+ * NULL, and must be for RV_NORM_NONE.  n_tokens 0 sets them to zero.  The outputs must not overlap the
+ * inputs.  rv_init must have run on the device: the sums' partial results lie in its workspace.  (dQ, dK, dV
+ * come from the caller: the library forms no gradient of the attention.) */
 rv_status rv_prepare_qkv_bwd(const rv_qkv_prep *p, const void *q, int64_t q_stride, const void *k,
                              int64_t k_stride, rv_dtype dtype, int n_tokens, const int32_t *pos, const void *dQ,
                              const void *dK, const void *dV, void *dq, int64_t dq_stride, void *dk,
@@ -389,7 +391,9 @@ rv_status rv_prepare_qkv_bwd(const rv_qkv_prep *p, const void *q, int64_t q_stri
  * failure nothing changes (RV_ERR_HIP from a launch excepted).  The calls allocate nothing and can be
  * captured.  A captured call repeats what it was enqueued with, lengths, rows and pages; it stays valid
  * while the sequences it names keep those pages (are not closed, compacted, or cut below those lengths)
- * and no other call writes the same rows.  Values are taken to be finite; rows past a sequence's end may
+ * and no other call writes the same rows.  A captured rv_pool_compact, and an append that copies a shared page,
+ * read pages that may be free once the call was enqueued: such a graph is replayed before another call takes pages.
+ * Values are taken to be finite; rows past a sequence's end may
  * hold anything.  One call moves at most 2^28 rows x heads of one sequence. */
 #define RV_PAGE_ROWS 64
 typedef struct rv_pool_s *rv_pool;
@@ -502,7 +506,9 @@ int rv_attention_plan_long(const rv_attn_plan *plan);
  * allocates; plans forced through RV_ATTN_SPLIT may need more -- and the saliency
  * staging that rv_admit_layers* use when the caller passes no saliency output, for up to
  * n_layers layers per call.  The workspace never shrinks.  Synchronises the device when
- * it replaces a buffer. */
+ * it replaces a buffer; graphs captured before then hold the old one (rv_attend_frame,
+ * rv_attend_frame_fused, rv_attend_staged, rv_admit_layers*, rv_prepare_qkv_bwd) and must
+ * be captured again. */
 rv_status rv_reserve_workspace(int n_tokens, int n_heads, int64_t max_mem_len, int n_layers);
 
 #ifdef __cplusplus

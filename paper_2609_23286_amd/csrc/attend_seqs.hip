@@ -12,11 +12,12 @@
 // A query tile has 128 rows, 32 a wave, over key tiles that the workgroup loads together (as attend.hip's core), or
 // 32 where a pass has no more, each wave taking key tiles of its own and no barrier among them.  What bounds them:
 // many queries, the core's stalls (attend.hip): four sequences' frames of 1041 tokens over 5000 shared rows and 100 to
-// 430 of their own 148 us, 728 TFLOP/s; one frame over 52,000 rows 290 us.  Few queries, memory, and over shared rows
-// both: 48 sequences of 5 tokens over 52,000 shared rows and 242 to 1041 of their own 106 us (at a large copy's rate
+// 430 of their own 146 us, 736 TFLOP/s; one frame over 52,000 rows 271 us.  Few queries, memory, and over shared rows
+// both: 48 sequences of 5 tokens over 52,000 shared rows and 242 to 1041 of their own 105 us (at a large copy's rate
 // the bytes, 340 MB, are 66; at the core's rate the 240 rows over the shared pages are 60 and the others' bytes 25).
-// A token each of 16 sequences, latency: 18 us, 13 of them the forward launch (3.6 until a workgroup has its place, 2
-// for the first keys, the rest two or three tiles and the write of the sums), 5 the merge.
+// A token each of 16 sequences over 10,000 rows of its own, 655 MB: 118 us, 5.6 TB/s; over 9990 shared rows, latency:
+// 18 us, 13 of them the forward launch (3.6 until a workgroup has its place, 2 for the first keys, the rest two or
+// three tiles and the write of the sums), 5 the merge.
 #include <type_traits>
 
 #include "attn_tile.h"

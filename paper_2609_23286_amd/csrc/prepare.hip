@@ -8,9 +8,10 @@
 // number's bits 1 and 2 change places.  The multiply-add reads the partner through a lane exchange, and the
 // norm's sums are 8 adds and three exchanges.  Eight heads fill a wave.  A wave takes a token (or a few, where
 // they have fewer than eight heads): its rows (token, head) of queries, of keys and of values are requested at
-// once, eight to an instruction.  Few registers are held per lane, so that the waves a CU holds cover the
-// latency of memory, which bounds it.  Results are written past the caches' reuse (nontemporal: 8328 tokens of
-// 16 heads 24.5 -> 19.6 us, 5.2 TB/s; the attention that follows takes the same time).
+// once, eight to an instruction.  Forward, a lane holds 67 to 109 registers, so that the four to seven waves a SIMD
+// cover the latency of memory, which bounds it; backward 161 to 214, two or three waves, each with more rows on their
+// way.  Results are written past the caches' reuse (nontemporal: 8328 tokens of 16 heads 24.5 -> 19.6 us when it was
+// taken; now 18.5 us, 5.5 TB/s, from fp32 25.7 us, 6.0 TB/s; the attention that follows takes the same time).
 //
 // Angles.  A token's position gives 32 distinct (axis, frequency) pairs whatever its head count, so
 // each lane of the wave forms one pair's sine and cosine and the heads read them from LDS.  The

@@ -605,7 +605,8 @@ def prepare_qkv_bwd(prep, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight=None, dq_
                     dk_bias=None, stream=None):
     """rv_prepare_qkv_bwd: the gradients dq, dk, dv of prepare_qkv's inputs (their dtype, rows at any
     distance) and, where given, of the weights and biases ([64] fp32, overwritten), from dQ [N, Hq, 64]
-    and dK, dV [N, Hk, 64] bf16.  dV and dv may be None."""
+    and dK, dV [N, Hk, 64] bf16.  dV and dv may be None.  No call here is recorded by autograd: a program's own
+    torch.autograd.Function calls this one."""
     device, s = _where(stream)
     prep._check_device(device)
     if _made(_bind.prepare_bwd(*prep._args, device, s, q, k, pos, dQ, dK, dV, dq, dk, dv, dq_weight, dq_bias,
